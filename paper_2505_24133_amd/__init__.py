@@ -16,6 +16,7 @@ _BINDING_NAMES = (
     "RKV_OK", "RKV_STATIC_SCRATCH_BYTES", "RkvError", "RkvParams", "Shape", "load_library", "make_workspace",
     "rkv_compact", "rkv_compact_inplace", "rkv_compress", "rkv_compress_inplace", "rkv_compress_static", "rkv_probe_mfma",
     "rkv_score_importance", "rkv_score_redundancy", "rkv_select_topk", "rkv_workspace_size", "status_string",
+    "make_attend_workspace", "rkv_attend", "rkv_attend_shared", "rkv_attend_workspace_size", "rkv_cache_append_rotary", "rotary_tables",
 )
 
 

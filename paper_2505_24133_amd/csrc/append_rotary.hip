@@ -1,0 +1,114 @@
+// New tokens on their way into the cache: keys and queries rotated by their positions, keys and values written behind the rows that are
+// held, the last queries into the query cache.  A workgroup has one token; a thread has 32 bytes of a row: a pair of 16-byte pieces
+// whose channels are rotated with each other (or 16 neighbouring channels of an interleaved row), so that a row's rotation stays inside
+// a thread and q_out may be q_new.  Every byte is read once and written once (twice where a query is kept): bound by memory, and for
+// single tokens by the three loads that follow each other (starts, row and position, page).
+#include "attend_internal.h"
+
+namespace rkv {
+
+namespace {
+
+struct Piece { uint32_t u[8]; };       // 16 channels: lower 8, upper 8
+
+__device__ __forceinline__ float lo_of(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float hi_of(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  union { bf16x2 b; uint32_t u; } r;
+  r.b = bf16x2{(__bf16)x, (__bf16)y};
+  return r.u;
+}
+
+__device__ __forceinline__ void turn(Piece& x, const float* c, const float* s, bool interleaved) {
+  float cs[8], sn[8];
+  *reinterpret_cast<float4*>(cs) = reinterpret_cast<const float4*>(c)[0];
+  *reinterpret_cast<float4*>(cs + 4) = reinterpret_cast<const float4*>(c)[1];
+  *reinterpret_cast<float4*>(sn) = reinterpret_cast<const float4*>(s)[0];
+  *reinterpret_cast<float4*>(sn + 4) = reinterpret_cast<const float4*>(s)[1];
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float a = lo_of(x.u[i]), b = hi_of(x.u[i]);
+      x.u[i] = pack2(a * cs[i] - b * sn[i], b * cs[i] + a * sn[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a0 = lo_of(x.u[i]), a1 = hi_of(x.u[i]), b0 = lo_of(x.u[4 + i]), b1 = hi_of(x.u[4 + i]);
+      x.u[i] = pack2(a0 * cs[2 * i] - b0 * sn[2 * i], a1 * cs[2 * i + 1] - b1 * sn[2 * i + 1]);
+      x.u[4 + i] = pack2(b0 * cs[2 * i] + a0 * sn[2 * i], b1 * cs[2 * i + 1] + a1 * sn[2 * i + 1]);
+    }
+  }
+}
+
+__device__ __forceinline__ Piece load(const uint16_t* row, int c0, int c1) {
+  Piece x;
+  *reinterpret_cast<uint4*>(x.u) = *reinterpret_cast<const uint4*>(row + c0 * 8);
+  *reinterpret_cast<uint4*>(x.u + 4) = *reinterpret_cast<const uint4*>(row + c1 * 8);
+  return x;
+}
+__device__ __forceinline__ void store(uint16_t* row, int c0, int c1, const Piece& x) {
+  *reinterpret_cast<uint4*>(row + c0 * 8) = *reinterpret_cast<const uint4*>(x.u);
+  *reinterpret_cast<uint4*>(row + c1 * 8) = *reinterpret_cast<const uint4*>(x.u + 4);
+}
+
+__global__ __launch_bounds__(256) void append_rotary_kernel(RotaryArgs a) {
+  const int t = blockIdx.x;
+  const int at = count_not_above(a.starts, a.P + 1, t) - 1;
+  if (at < 0 || at >= a.P) return;                       // a token of no problem
+  const int j = t - a.starts[at];
+  const int row = a.held[at] + j, position = a.seen[at] + j;
+  const bool kept = a.q_cache != nullptr && t >= a.starts[at + 1] - a.alpha;
+  int64_t k_at = -1, v_at = -1;                          // where the row lies in the caches; -1: nowhere
+  if (row >= 0 && row < a.N) {
+    if (a.kl.table == nullptr) {
+      k_at = at * a.kl.sp + row * a.kl.st;
+      v_at = at * a.vl.sp + row * a.vl.st;
+    } else {
+      const int page = a.kl.table[(int64_t)at * a.kl.table_stride + (row >> a.kl.page_shift)];
+      const int slot = row & ((1 << a.kl.page_shift) - 1);
+      if (page >= 0 && page < a.num_pages) {
+        k_at = page * a.kl.spage + slot * a.kl.st;
+        v_at = page * a.vl.spage + slot * a.vl.st;
+      }
+    }
+  }
+  const int angle = min(max(position, 0), a.table_rows - 1);
+  const int half = a.rotary / 2;
+  int slot = position % a.alpha;
+  if (slot < 0) slot += a.alpha;
+  const int units = (a.Hq + 2 * a.H) * 8;
+  for (int u = threadIdx.x; u < units; u += 256) {
+    const int head = u >> 3, piece = u & 7, pairs = a.rotary >> 4;      // pairs of pieces that are rotated
+    const bool turned = piece < pairs;
+    const int c0 = a.interleaved || !turned ? 2 * piece : piece, c1 = a.interleaved || !turned ? 2 * piece + 1 : piece + pairs;
+    const float* c = a.cos + (int64_t)angle * half + piece * 8;
+    const float* s = a.sin + (int64_t)angle * half + piece * 8;
+    if (head < a.Hq) {
+      Piece x = load(a.q_new + t * a.qnt + head * a.qnh, c0, c1);
+      if (turned) turn(x, c, s, a.interleaved);
+      store(a.q_out + t * a.qot + head * a.qoh, c0, c1, x);
+      if (kept) store(a.q_cache + at * a.qsp + head * a.qsh + slot * a.qst, c0, c1, x);
+    } else if (head < a.Hq + a.H) {
+      const int h = head - a.Hq;
+      if (k_at < 0) continue;
+      Piece x = load(a.k_new + t * a.knt + h * a.knh, c0, c1);
+      if (turned) turn(x, c, s, a.interleaved);
+      store(a.k_cache + k_at + h * a.kl.sh, c0, c1, x);
+    } else {
+      const int h = head - a.Hq - a.H;
+      if (v_at < 0) continue;
+      store(a.v_cache + v_at + h * a.vl.sh, c0, c1, load(a.v_new + t * a.vnt + h * a.vnh, c0, c1));
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_append_rotary(const RotaryArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(append_rotary_kernel, dim3(a.T), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace rkv

@@ -1,0 +1,239 @@
+// C ABI of rkv_attend.h: argument validation, how the work is cut, workspace carve-up and kernel sequencing.
+#include <math.h>
+
+#include <algorithm>
+
+#include "attend_internal.h"
+
+namespace rkv {
+
+int64_t attend_tile_bound(int64_t T, int G, int64_t owners);
+
+namespace {
+
+constexpr int kMaxTokens = 1 << 24;
+constexpr int64_t kMaxBlocks = 1 << 23;
+constexpr int kSlots = 512;                 // workgroups that the chip's 256 compute units hold of the kernel for many rows
+
+bool row_stride(int64_t s) { return s >= kHeadDim && s <= 32768 && s % 8 == 0; }
+bool wide_stride(int64_t s, bool several) { return s >= 0 && s % 8 == 0 && (s > 0 || !several); }
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// The caches as rkv_params describes them, checked as the compression step checks them.
+struct Caches {
+  int P, H, G, N;
+  bool paged;
+  KvLayout kl, vl;
+};
+
+rkv_status read_caches(const rkv_params& q, int num_pages, Caches* c) {
+  if (q.num_problems < 0 || q.kv_heads < 1 || q.q_heads < 1 || q.n_tokens < 1 || q.q_heads % q.kv_heads != 0) return RKV_ERR_SHAPE;
+  if (q.head_dim != kHeadDim || q.n_tokens > kMaxTokens || q.q_heads > 4096 || (int64_t)q.num_problems * q.kv_heads > (1 << 22)) return RKV_ERR_UNSUPPORTED;
+  c->P = q.num_problems; c->H = q.kv_heads; c->G = q.q_heads / q.kv_heads; c->N = q.n_tokens;
+  c->paged = q.page_size != 0;
+  int shift = 0;
+  if (c->paged) {
+    if (q.page_size != 16 && q.page_size != 32 && q.page_size != 64 && q.page_size != 128) return RKV_ERR_UNSUPPORTED;
+    while ((1 << shift) < q.page_size) ++shift;
+    if (q.num_problems > 0 && q.block_table == nullptr) return RKV_ERR_NULL;
+    if ((int64_t)q.table_stride * q.page_size < q.n_tokens || num_pages < 1) return RKV_ERR_SHAPE;
+  }
+  auto layout = [&](int64_t sp, int64_t sh, int64_t st, int64_t spage, KvLayout* l) {
+    if (!c->paged && sp == 0 && sh == 0 && st == 0) {
+      st = kHeadDim; sh = (int64_t)q.n_tokens * kHeadDim; sp = sh * q.kv_heads;
+    }
+    *l = KvLayout{c->paged ? q.block_table : nullptr, shift, q.table_stride, sp, sh, st, spage};
+    return row_stride(st) && wide_stride(sh, q.kv_heads > 1) && (c->paged ? spage > 0 && spage % 8 == 0 : wide_stride(sp, q.num_problems > 1));
+  };
+  if (!layout(q.k_stride_problem, q.k_stride_head, q.k_stride_token, q.k_stride_page, &c->kl) ||
+      !layout(q.v_stride_problem, q.v_stride_head, q.v_stride_token, q.v_stride_page, &c->vl))
+    return RKV_ERR_SHAPE;
+  return RKV_OK;
+}
+
+// Strides of an array [T, heads, d]; 0, 0 = dense.
+bool token_strides(int64_t st, int64_t sh, int heads, int64_t tokens, int64_t* ot, int64_t* oh) {
+  if (st == 0 && sh == 0) { *oh = kHeadDim; *ot = (int64_t)heads * kHeadDim; return true; }
+  *ot = st; *oh = sh;
+  return wide_stride(st, tokens > 1) && wide_stride(sh, heads > 1) && st <= (int64_t)1 << 40 && sh <= (int64_t)1 << 40;
+}
+
+struct AttendPlan {
+  AttendArgs a;
+  bool paged;
+  size_t off_small_o, off_small_ml, off_tile_o, off_tile_ml, off_prefix_o, off_prefix_ml, total;
+};
+
+int split_over(int64_t blocks, int64_t slots, int64_t most) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>((slots + blocks - 1) / std::max<int64_t>(blocks, 1), most));
+}
+
+rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool shared, AttendPlan* pl) {
+  if (prm == nullptr || att == nullptr) return RKV_ERR_NULL;
+  const rkv_attend_params& t = *att;
+  Caches c;
+  const rkv_status s = read_caches(*prm, t.num_pages, &c);
+  if (s != RKV_OK) return s;
+  if (t.tokens < 0 || (t.tokens > 0 && (t.max_new < 1 || t.max_new > t.tokens))) return RKV_ERR_SHAPE;
+  if (t.groups < 0 || t.groups > c.P || (!shared && t.groups != 0)) return RKV_ERR_SHAPE;
+  if (t.tokens > kMaxTokens || (int64_t)t.tokens * c.H * c.G > 0x7fffffff) return RKV_ERR_UNSUPPORTED;
+  if (t.window < 0 || t.sinks < 0 || !(t.scale > 0.f) || !isfinite(t.scale)) return RKV_ERR_PARAM;
+  AttendArgs& a = pl->a;
+  a = AttendArgs{};
+  if (!token_strides(t.q_stride_token, t.q_stride_head, c.H * c.G, t.tokens, &a.qst, &a.qsh) ||
+      !token_strides(t.o_stride_token, t.o_stride_head, c.H * c.G, t.tokens, &a.ost, &a.osh))
+    return RKV_ERR_SHAPE;
+  a.starts = t.starts; a.kv_len = t.kv_len; a.group_starts = t.group_starts; a.prefix_len = t.prefix_len;
+  a.P = c.P; a.H = c.H; a.G = c.G; a.N = c.N; a.T = t.tokens; a.groups = t.groups;
+  a.window = t.window; a.sinks = t.sinks; a.num_pages = t.num_pages;
+  a.kl = c.kl; a.vl = c.vl;
+  a.scale2 = t.scale * 1.4426950408889634f;
+  pl->paged = c.paged;
+  pl->total = 0;
+  if (c.P == 0 || t.tokens == 0) return RKV_OK;
+
+  // Which kernels run.  Up to 64 rows of queries per KV head (new tokens * G) the few-rows kernel has them; where a problem may have
+  // more, the many-rows kernel has those problems, and the few-rows kernel the others if there are any.
+  const int64_t most_rows = (int64_t)t.max_new * c.G;
+  const bool large = most_rows > kSmallRows;
+  const bool small = !large || (c.P > 1 && c.G <= kSmallRows);
+  // rows that a query may see, at most
+  const int64_t reach = t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + t.max_new) : c.N;
+  // A unit's rows are dealt to several workgroups where there are fewer units than the chip takes at once (256 and 512)
+  if (small) {
+    a.small_rows = large || most_rows > 32 ? 64 : (most_rows > 16 ? 32 : 16);
+    a.small_splits = split_over((int64_t)c.P * c.H, 256, (reach + 127) / 128);
+  }
+  if (large) a.tile_splits = split_over(attend_tile_bound(t.tokens, c.G, c.P) * c.H, kSlots, std::min<int64_t>((reach + 255) / 256, 32));
+  if (t.groups > 0) a.prefix_splits = split_over(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, kSlots, std::min<int64_t>((reach + 255) / 256, 32));
+  if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
+      attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
+      (int64_t)t.tokens * ((c.H * c.G + 7) / 8) > kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)
+    return RKV_ERR_UNSUPPORTED;
+
+  auto take = [&](int64_t bytes) {
+    const size_t o = pl->total;
+    pl->total = (o + (size_t)bytes + 255) & ~(size_t)255;
+    return o;
+  };
+  const int64_t rows = (int64_t)t.tokens * c.H * c.G;
+  const int64_t small_parts = a.small_splits > 1 || (small && t.groups > 0) ? (int64_t)c.P * c.H * a.small_rows * a.small_splits : 0;
+  const int64_t tile_parts = a.tile_splits > 1 || (large && t.groups > 0) ? rows * a.tile_splits : 0;
+  const int64_t prefix_parts = rows * a.prefix_splits;
+  pl->off_small_o = take(small_parts * kHeadDim * 4);
+  pl->off_small_ml = take(small_parts * 8);
+  pl->off_tile_o = take(tile_parts * kHeadDim * 4);
+  pl->off_tile_ml = take(tile_parts * 8);
+  pl->off_prefix_o = take(prefix_parts * kHeadDim * 4);
+  pl->off_prefix_ml = take(prefix_parts * 8);
+  return RKV_OK;
+}
+
+rkv_status attend(const rkv_params* prm, const rkv_attend_params* att, bool shared, const void* q, const void* k, const void* v,
+                  void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  AttendPlan pl;
+  const rkv_status s = plan_attend(prm, att, shared, &pl);
+  if (s != RKV_OK) return s;
+  AttendArgs& a = pl.a;
+  if (a.P == 0 || a.T == 0) return RKV_OK;
+  if (q == nullptr || k == nullptr || v == nullptr || out == nullptr || a.starts == nullptr || a.kv_len == nullptr ||
+      (a.groups > 0 && (a.group_starts == nullptr || a.prefix_len == nullptr)))
+    return RKV_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return RKV_ERR_SHAPE;
+  if (pl.total > 0 && (ws == nullptr || ((uintptr_t)ws & 255) != 0 || ws_bytes < pl.total)) return RKV_ERR_WORKSPACE;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  char* w = static_cast<char*>(ws);
+  a.small_o = reinterpret_cast<float*>(w + pl.off_small_o);
+  a.small_ml = reinterpret_cast<float2*>(w + pl.off_small_ml);
+  a.tile_o = reinterpret_cast<float*>(w + pl.off_tile_o);
+  a.tile_ml = reinterpret_cast<float2*>(w + pl.off_tile_ml);
+  a.prefix_o = reinterpret_cast<float*>(w + pl.off_prefix_o);
+  a.prefix_ml = reinterpret_cast<float2*>(w + pl.off_prefix_ml);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (a.prefix_splits > 0 && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
+  if (a.tile_splits > 0 && launch_attend_tiles(a, pl.paged, false, st) != hipSuccess) return RKV_ERR_HIP;
+  if (a.small_splits > 0 && launch_attend_small(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
+  // parts of single tokens alone are joined unit by unit; where many-rows parts or prefixes are to be joined, token by token
+  const bool per_token = a.prefix_splits > 0 || a.tile_splits > 1;
+  if ((per_token || a.small_splits > 1) && launch_attend_join(a, per_token, st) != hipSuccess) return RKV_ERR_HIP;
+  return RKV_OK;
+}
+
+}  // namespace
+}  // namespace rkv
+
+using namespace rkv;
+
+extern "C" {
+
+rkv_status rkv_attend_workspace_size(const rkv_params* prm, const rkv_attend_params* att, size_t* bytes) {
+  if (bytes == nullptr) return RKV_ERR_NULL;
+  AttendPlan pl;
+  const rkv_status s = plan_attend(prm, att, true, &pl);
+  if (s == RKV_OK) *bytes = pl.total;
+  return s;
+}
+
+rkv_status rkv_attend(const rkv_params* prm, const rkv_attend_params* att, const void* q, const void* k, const void* v,
+                      void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return attend(prm, att, false, q, k, v, out, lse, ws, ws_bytes, stream);
+}
+
+rkv_status rkv_attend_shared(const rkv_params* prm, const rkv_attend_params* att, const void* q, const void* k, const void* v,
+                             void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return attend(prm, att, true, q, k, v, out, lse, ws, ws_bytes, stream);
+}
+
+rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_params* rot, void* k_cache, void* v_cache, void* q_cache,
+                                   const void* k_new, const void* v_new, const void* q_new, void* q_out, void* stream) {
+  if (prm == nullptr || rot == nullptr) return RKV_ERR_NULL;
+  const rkv_rotary_params& r = *rot;
+  Caches c;
+  const rkv_status s = read_caches(*prm, r.num_pages, &c);
+  if (s != RKV_OK) return s;
+  const int Hq = c.H * c.G;
+  if (r.tokens < 0 || r.table_rows < 1) return RKV_ERR_SHAPE;
+  if (r.tokens > kMaxTokens / 2 || r.rotary_dim < 16 || r.rotary_dim > kHeadDim || r.rotary_dim % 16 != 0) return RKV_ERR_UNSUPPORTED;
+  if (r.interleaved != 0 && r.interleaved != 1) return RKV_ERR_PARAM;
+  RotaryArgs a = {};
+  if (!token_strides(r.k_stride_token, r.k_stride_head, c.H, r.tokens, &a.knt, &a.knh) ||
+      !token_strides(r.v_stride_token, r.v_stride_head, c.H, r.tokens, &a.vnt, &a.vnh) ||
+      !token_strides(r.q_stride_token, r.q_stride_head, Hq, r.tokens, &a.qnt, &a.qnh) ||
+      !token_strides(r.o_stride_token, r.o_stride_head, Hq, r.tokens, &a.qot, &a.qoh))
+    return RKV_ERR_SHAPE;
+  a.alpha = 1;
+  if (q_cache != nullptr) {
+    if (prm->alpha < 1) return RKV_ERR_SHAPE;
+    a.alpha = prm->alpha;
+    a.qsp = prm->q_stride_problem; a.qsh = prm->q_stride_head; a.qst = prm->q_stride_token;
+    if (a.qsp == 0 && a.qsh == 0 && a.qst == 0) {
+      a.qst = kHeadDim; a.qsh = (int64_t)a.alpha * kHeadDim; a.qsp = a.qsh * Hq;
+    }
+    if (a.qst < kHeadDim || a.qst % 8 != 0 || !wide_stride(a.qsh, Hq > 1) || !wide_stride(a.qsp, c.P > 1)) return RKV_ERR_SHAPE;
+  }
+  if (c.P == 0 || r.tokens == 0) return RKV_OK;
+  if (k_cache == nullptr || v_cache == nullptr || k_new == nullptr || v_new == nullptr || q_new == nullptr || q_out == nullptr ||
+      r.cos == nullptr || r.sin == nullptr || r.starts == nullptr || r.held == nullptr || r.seen == nullptr)
+    return RKV_ERR_NULL;
+  for (const void* x : {(const void*)k_cache, (const void*)v_cache, (const void*)q_cache, k_new, v_new, q_new, (const void*)q_out,
+                        (const void*)r.cos, (const void*)r.sin})
+    if (!aligned16(x)) return RKV_ERR_SHAPE;
+  a.k_cache = static_cast<uint16_t*>(k_cache);
+  a.v_cache = static_cast<uint16_t*>(v_cache);
+  a.q_cache = static_cast<uint16_t*>(q_cache);
+  a.k_new = static_cast<const uint16_t*>(k_new);
+  a.v_new = static_cast<const uint16_t*>(v_new);
+  a.q_new = static_cast<const uint16_t*>(q_new);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.cos = r.cos; a.sin = r.sin; a.starts = r.starts; a.held = r.held; a.seen = r.seen;
+  a.P = c.P; a.H = c.H; a.Hq = Hq; a.N = c.N; a.T = r.tokens;
+  a.rotary = r.rotary_dim; a.interleaved = r.interleaved; a.table_rows = r.table_rows; a.num_pages = r.num_pages;
+  a.kl = c.kl; a.vl = c.vl;
+  return launch_append_rotary(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RKV_OK : RKV_ERR_HIP;
+}
+
+}  // extern "C"

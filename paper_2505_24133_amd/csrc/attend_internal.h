@@ -1,0 +1,242 @@
+// Shared parts of the attention kernels over the cache (gfx950): which rows a block of queries reads, how rows are found and
+// copied to LDS, and the one-pass softmax.
+//
+// For a query q with visible rows c:  s_c = scale log2(e) q . k_c,  M = max s_c,  l = sum 2^(s_c - M),  o = sum 2^(s_c - M) v_c / l.
+// M, l and the unnormalised o are carried over the rows; a part of the rows is described by its (M, l, o), and parts are joined by
+// M = max M_i, weights 2^(M_i - M).  A part without a visible row has M = -inf, l = 0.
+#pragma once
+
+#include <math.h>
+
+#include "rkv_attend.h"
+#include "rkv_internal.h"
+
+namespace rkv {
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+
+constexpr int kSmallRows = 64;       // query rows per KV head (new tokens * G) that the kernel for few rows takes at most
+constexpr int kTileRows = 128;       // query rows of a tile of the kernel for many
+
+struct AttendArgs {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* out;
+  float* lse;                  // or nullptr
+  const int32_t* starts;
+  const int32_t* kv_len;
+  const int32_t* group_starts; // groups > 0: problems that share their first rows
+  const int32_t* prefix_len;
+  int P, H, G, N, T, groups, window, sinks, num_pages;
+  KvLayout kl, vl;
+  int64_t qst, qsh, ost, osh;
+  float scale2;                // scale * log2(e)
+  // parts of the rows, unnormalised: few-rows kernel [p][split][h][small_rows], many-rows kernel [split][t][hq], prefixes likewise
+  int small_splits, tile_splits, prefix_splits;   // 0: the kernel does not run
+  int small_rows;              // rows per unit in the few-rows parts
+  float* small_o;
+  float2* small_ml;
+  float* tile_o;
+  float2* tile_ml;
+  float* prefix_o;
+  float2* prefix_ml;
+};
+
+// ------------------------------------------------------------------------------------------------ which rows
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+// Number of entries of the ascending array a[0 .. n) that are <= t; t is the same in all lanes.  64 of them are compared at a time.
+__device__ __forceinline__ int count_not_above(const int32_t* a, int n, int t) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, len = n;
+  while (len > 0) {
+    const int step = (len + 63) >> 6;
+    const int at = (lane + 1) * step - 1;
+    const bool le = at < len && a[lo + min(at, len - 1)] <= t;
+    const int c = __popcll(__ballot(le));
+    lo += c * step;
+    if (step == 1) break;
+    len = min(step, len - c * step);
+  }
+  return lo;
+}
+
+struct Tokens { int first, count; };       // of a problem, or of a group
+__device__ __forceinline__ Tokens tokens_between(const AttendArgs& a, int p0, int p1) {
+  const int lo = clampi(a.starts[p0], 0, a.T), hi = clampi(a.starts[p1], 0, a.T);
+  return Tokens{lo, max(hi - lo, 0)};
+}
+// The group that problem p belongs to, or -1.  (uniform)
+__device__ __forceinline__ int group_of(const AttendArgs& a, int p) {
+  if (a.groups == 0) return -1;
+  const int g = count_not_above(a.group_starts, a.groups + 1, p) - 1;
+  return g >= 0 && g < a.groups ? g : -1;
+}
+__device__ __forceinline__ int prefix_of(const AttendArgs& a, int g) { return g < 0 ? 0 : clampi(a.prefix_len[g], 0, a.N); }
+
+// What the token at row r of its problem may see: rows c < hi with c >= lo or c < sinks.
+struct Sight { int lo, hi; };
+__device__ __forceinline__ Sight sight(const AttendArgs& a, int r) {
+  return Sight{a.window > 0 ? max(r - a.window + 1, 0) : 0, max(r + 1, 0)};
+}
+
+// The rows of [base, lim) that a block of queries reads, in tiles of TK: those before `sinks` and those from the lowest lo on.
+template <int TK>
+struct Span {
+  int start_a, end_a, tiles_a, start_b, end_b, tiles;
+  __device__ __forceinline__ Span(int base, int lim, int lo_min, int hi_max, int sinks) {
+    end_b = min(hi_max, lim);
+    start_b = max(base, lo_min);
+    start_a = base;
+    end_a = min(min(sinks, lim), hi_max);
+    if (end_a >= start_b) { start_b = base; end_a = base; }
+    tiles_a = end_a > start_a ? (end_a - start_a + TK - 1) / TK : 0;
+    tiles = tiles_a + (end_b > start_b ? (end_b - start_b + TK - 1) / TK : 0);
+  }
+  __device__ __forceinline__ int start(int i) const { return i < tiles_a ? start_a + i * TK : start_b + (i - tiles_a) * TK; }
+  __device__ __forceinline__ int end(int i) const { return i < tiles_a ? end_a : end_b; }
+};
+
+// --------------------------------------------------------------------------------------------- where rows lie
+// Rows of one problem and head.  Paged: the ids of 64 consecutive pages lie in the lanes of the wave (1024 rows and more), and a
+// row's page is fetched from its lane; reload() is called with wave-uniform rows before rows are looked up.
+template <bool PAGED>
+struct Rows {
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* table;
+  int shift, pages, num_pages, first, ids;
+  int64_t kst, vst, kspage, vspage;
+  __device__ __forceinline__ Rows(const AttendArgs& a, int p, int h) {
+    k = a.k + h * a.kl.sh;
+    v = a.v + h * a.vl.sh;
+    kst = a.kl.st; vst = a.vl.st;
+    if constexpr (PAGED) {
+      shift = a.kl.page_shift;
+      pages = (a.N + (1 << shift) - 1) >> shift;
+      num_pages = a.num_pages;
+      table = a.kl.table + (int64_t)p * a.kl.table_stride;
+      kspage = a.kl.spage; vspage = a.vl.spage;
+      first = -64;
+      ids = 0;
+    } else {
+      k += p * a.kl.sp;
+      v += p * a.vl.sp;
+    }
+  }
+  __device__ __forceinline__ void reload(int row_lo, int row_hi) {
+    if constexpr (PAGED) {
+      const int lo = row_lo >> shift, hi = row_hi >> shift;
+      if (lo < first || hi >= first + 64) {
+        first = lo;
+        ids = clampi(table[min(lo + (int)(threadIdx.x & 63), pages - 1)], 0, num_pages - 1);
+      }
+    }
+  }
+  // Addresses of 16-byte piece ck of row's key and piece cv of its value.
+  __device__ __forceinline__ void find(int row, int ck, int cv, const uint16_t** kp, const uint16_t** vp) const {
+    if constexpr (PAGED) {
+      const int page = __builtin_amdgcn_ds_bpermute(((row >> shift) - first) << 2, ids);
+      const int slot = row & ((1 << shift) - 1);
+      *kp = k + page * kspage + slot * kst + ck * 8;
+      *vp = v + page * vspage + slot * vst + cv * 8;
+    } else {
+      *kp = k + row * kst + ck * 8;
+      *vp = v + row * vst + cv * 8;
+    }
+  }
+};
+
+// One wave-wide copy of 64 x 16 bytes from an address per lane to consecutive places in LDS (see dma16 for why it is written out).
+__device__ __forceinline__ void dma16_from(const uint16_t* from, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_base), "v"(from) : "memory", "m0");
+}
+
+// Places in LDS of 16-byte piece `chunk` of row `row`: keys are read 16 rows at one chunk (the four low bits of the row spread
+// them over all banks), values four rows at two neighbouring chunks, transposed (pairs of chunks are spread by three bits of the row).
+__device__ __forceinline__ int key_chunk(int row, int chunk) { return chunk ^ (row & 15); }
+__device__ __forceinline__ int value_chunk(int row, int chunk) { return chunk ^ ((row & 7) << 1); }
+
+// Four rows of one channel: lane i of 16 gets channel i of the 16 channels whose four rows the lanes address, lane 4 m + n the
+// 8 bytes of row m, channels 4 n .. 4 n + 3.
+__device__ __forceinline__ s16x4 read_transposed(uint32_t lds_address) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)lds_address);
+}
+
+// ------------------------------------------------------------------------------------------ infinities and NaN
+// A hidden row's weight is 0, and 0 times infinity is NaN: where some query does not see a row of a tile, values that are not finite
+// are taken out of the product, and the queries that give them weight get them added afterwards.
+union Frag {
+  bf16x8 b;
+  uint32_t u[4];
+  s16x4 s[2];
+};
+__device__ __forceinline__ uint32_t not_finite(const Frag& f) {      // bit 15 or 31 of the result is set if an element is not finite
+  uint32_t acc = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc |= (f.u[i] & 0x7f807f80u) + 0x00800080u;
+  return acc & 0x80008000u;
+}
+// f without what is not finite; up: 1 where f is +inf or NaN; down: 1 where it is -inf or NaN.
+__device__ __forceinline__ void split_not_finite(Frag& f, Frag& up, Frag& down) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t keep = 0, u = 0, d = 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t x = (f.u[i] >> (16 * half)) & 0xffffu;
+      const bool bad = (x & 0x7f80u) == 0x7f80u, nan = bad && (x & 0x7fu) != 0;
+      keep |= (bad ? 0u : x) << (16 * half);
+      u |= (bad && (nan || x < 0x8000u) ? 0x3f80u : 0u) << (16 * half);
+      d |= (bad && (nan || x >= 0x8000u) ? 0x3f80u : 0u) << (16 * half);
+    }
+    f.u[i] = keep; up.u[i] = u; down.u[i] = d;
+  }
+}
+__device__ __forceinline__ Frag given_weight(const Frag& p) {        // 1 where the weight is not 0
+  Frag r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.u[i] = ((p.u[i] & 0x7fffu) ? 0x3f80u : 0u) | ((p.u[i] & 0x7fff0000u) ? 0x3f800000u : 0u);
+  return r;
+}
+
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+// Subtrahend of the exponents: 0 as long as nothing is visible, so that 2^(-inf - M) is 0 and not NaN.
+__device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __log2f(l)) * 0.69314718055994531f : (l == 0.f ? -INFINITY : l); }
+
+// Four values as bf16, rounded to nearest even: the outputs' type.
+__device__ __forceinline__ uint2 pack4(float x, float y, float z, float w) {
+  typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
+  union { bf16x4 b; uint2 u; } r;
+  r.b = bf16x4{(__bf16)x, (__bf16)y, (__bf16)z, (__bf16)w};
+  return r.u;
+}
+
+hipError_t launch_attend_small(const AttendArgs& a, bool paged, hipStream_t stream);
+hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool prefix, hipStream_t stream);
+hipError_t launch_attend_join(const AttendArgs& a, bool per_token, hipStream_t stream);
+
+struct RotaryArgs {
+  uint16_t* k_cache;
+  uint16_t* v_cache;
+  uint16_t* q_cache;           // or nullptr
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  const uint16_t* q_new;
+  uint16_t* q_out;
+  const float* cos;
+  const float* sin;
+  const int32_t* starts;
+  const int32_t* held;
+  const int32_t* seen;
+  int P, H, Hq, N, T, alpha, rotary, interleaved, table_rows, num_pages;
+  KvLayout kl, vl;
+  int64_t qsp, qsh, qst;       // query cache: problem, head, slot
+  int64_t knt, knh, vnt, vnh, qnt, qnh, qot, qoh;
+};
+hipError_t launch_append_rotary(const RotaryArgs& a, hipStream_t stream);
+
+}  // namespace rkv

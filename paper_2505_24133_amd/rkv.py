@@ -54,6 +54,27 @@ class RkvParams(ctypes.Structure):
     ]
 
 
+class RkvRotaryParams(ctypes.Structure):
+    """Mirror of ``rkv_rotary_params``."""
+    _fields_ = [
+        ("tokens", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("table_rows", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("held", ctypes.c_void_p), ("seen", ctypes.c_void_p),
+        ("k_stride_token", ctypes.c_int64), ("k_stride_head", ctypes.c_int64), ("v_stride_token", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+        ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64), ("o_stride_token", ctypes.c_int64), ("o_stride_head", ctypes.c_int64),
+    ]
+
+
+class RkvAttendParams(ctypes.Structure):
+    """Mirror of ``rkv_attend_params``."""
+    _fields_ = [
+        ("tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+        ("groups", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("starts", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("group_starts", ctypes.c_void_p), ("prefix_len", ctypes.c_void_p),
+        ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64), ("o_stride_token", ctypes.c_int64), ("o_stride_head", ctypes.c_int64),
+    ]
+
+
 _PACK_PARAMS = struct.Struct("@9i3fI12q2iP2q").pack_into
 assert struct.calcsize("@9i3fI12q2iP2q") == ctypes.sizeof(RkvParams)
 
@@ -90,7 +111,11 @@ def load_library() -> ctypes.CDLL:
     lib.rkv_should_compress.argtypes = [P, ctypes.c_int32]
     lib.rkv_cache_append.argtypes = [P, V, V, V, V, V, V, ctypes.c_int32, ctypes.c_int32, V]
     lib.rkv_probe_mfma.argtypes = [V, V, ctypes.c_int, V, ctypes.POINTER(ctypes.c_int64)]
-    for name in ("rkv_workspace_size", "rkv_score_importance", "rkv_score_redundancy", "rkv_select_topk",
+    R, A = ctypes.POINTER(RkvRotaryParams), ctypes.POINTER(RkvAttendParams)
+    lib.rkv_cache_append_rotary.argtypes = [P, R, V, V, V, V, V, V, V, V]
+    lib.rkv_attend_workspace_size.argtypes = [P, A, ctypes.POINTER(S)]
+    lib.rkv_attend.argtypes = lib.rkv_attend_shared.argtypes = [P, A, V, V, V, V, V, V, S, V]
+    for name in ("rkv_cache_append_rotary", "rkv_attend_workspace_size", "rkv_attend", "rkv_attend_shared", "rkv_workspace_size", "rkv_score_importance", "rkv_score_redundancy", "rkv_select_topk",
                  "rkv_compact", "rkv_compress", "rkv_compress_events", "rkv_compress_static", "rkv_should_compress", "rkv_cache_append",
                  "rkv_compact_inplace", "rkv_compress_inplace", "rkv_probe_mfma"):
         getattr(lib, name).restype = ctypes.c_int
@@ -466,3 +491,159 @@ def rkv_compress_static(shape: Shape, q_obs: torch.Tensor, k: torch.Tensor, v: t
     if s < 0:
         raise RkvError(s, "rkv_compress_static")
     return s
+
+
+# ---------------------------------------------------------------------------- the decode loop around the step (rkv_attend.h)
+_INT32_MAX = 2 ** 31 - 1
+
+
+def rotary_tables(table_rows: int, rotary_dim: int = 128, base: float = 10000.0, device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
+    """cos and sin of position * base^(-2 i / rotary_dim), fp32 [table_rows, rotary_dim / 2]; the angles are formed in float64."""
+    rate = base ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64, device=device) / rotary_dim)
+    angle = torch.arange(table_rows, dtype=torch.float64, device=device)[:, None] * rate
+    return angle.cos().float(), angle.sin().float()
+
+
+def _need_here(*tensors: Optional[torch.Tensor]) -> None:
+    """GPU tensors, and of the device whose current stream the work is enqueued on."""
+    _need_gpu(*tensors)
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensors must be on the current device cuda:{here}, got {t.device}")
+
+
+def _check_tokens(t: torch.Tensor, want: Tuple[int, int, int], what: str) -> None:
+    if tuple(t.shape) != want or t.dtype != torch.bfloat16 or t.stride(2) != 1:
+        raise ValueError(f"{what} must be bf16 {want} with a contiguous last dimension, got {tuple(t.shape)} {t.dtype}")
+
+
+def _check_list(t: torch.Tensor, entries: int, what: str) -> None:
+    if tuple(t.shape) != (entries,) or t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 [{entries}], got {tuple(t.shape)} {t.dtype}")
+
+
+def _token_strides(t: torch.Tensor) -> Tuple[int, int]:
+    """Token and head strides in elements, 0 where there is one entry only (0, 0: dense)."""
+    if t.is_contiguous():
+        return 0, 0
+    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
+def _pages(shape: Shape, k: torch.Tensor, v: torch.Tensor) -> int:
+    if not shape.page_size:
+        return 0
+    return min(k.shape[0], v.shape[0])
+
+
+def rkv_cache_append_rotary(shape: Shape, k_cache: torch.Tensor, v_cache: torch.Tensor, q_cache: Optional[torch.Tensor],
+                            k_new: torch.Tensor, v_new: torch.Tensor, q_new: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor,
+                            starts: torch.Tensor, held: torch.Tensor, seen: torch.Tensor, interleaved: bool = False,
+                            q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotate a ragged batch of new tokens (k_new, v_new [T, kv_heads, d], q_new [T, q_heads, d]; starts cuts them into the problems') by
+    their positions seen[p] + j and write keys and values behind the held[p] rows of the caches and the last alpha queries of every
+    problem into q_cache (None: nowhere).  Returns the rotated queries (q_out, which may be q_new itself)."""
+    if q_out is None:
+        q_out = torch.empty(q_new.shape, dtype=q_new.dtype, device=q_new.device)
+    _need_here(k_cache, v_cache, q_cache, k_new, v_new, q_new, cos, sin, starts, held, seen, q_out)
+    _check_kv(shape, k_cache, "k_cache")
+    _check_kv(shape, v_cache, "v_cache")
+    if q_cache is not None:
+        _check_q(shape, q_cache)
+    T = k_new.shape[0]
+    kv, qs = (T, shape.kv_heads, shape.head_dim), (T, shape.q_heads, shape.head_dim)
+    for t, want, what in ((k_new, kv, "k_new"), (v_new, kv, "v_new"), (q_new, qs, "q_new"), (q_out, qs, "q_out")):
+        _check_tokens(t, want, what)
+    if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 \
+            or not cos.is_contiguous() or not sin.is_contiguous():
+        raise ValueError("cos and sin must be contiguous fp32 [table_rows, rotary_dim / 2]")
+    for t, entries, what in ((starts, shape.num_problems + 1, "starts"), (held, shape.num_problems, "held"), (seen, shape.num_problems, "seen")):
+        _check_list(t, entries, what)
+    prm = shape.params(k_cache, v_cache, q=q_cache)
+    rot = RkvRotaryParams(T, 2 * cos.shape[1], int(bool(interleaved)), cos.shape[0], _pages(shape, k_cache, v_cache), _ptr(cos), _ptr(sin),
+                          _ptr(starts), _ptr(held), _ptr(seen), *_token_strides(k_new), *_token_strides(v_new), *_token_strides(q_new),
+                          *_token_strides(q_out))
+    s = load_library().rkv_cache_append_rotary(ctypes.byref(prm), ctypes.byref(rot), _ptr(k_cache), _ptr(v_cache), _ptr(q_cache), _ptr(k_new),
+                                               _ptr(v_new), _ptr(q_new), _ptr(q_out), _stream())
+    if s != RKV_OK:
+        raise RkvError(s, "rkv_cache_append_rotary")
+    return q_out
+
+
+def rkv_attend_workspace_size(shape: Shape, tokens: int, max_new: Optional[int] = None, groups: int = 0, window: int = 0, sinks: int = 0) -> int:
+    """Bytes that rkv_attend (or, with groups, rkv_attend_shared) needs for `tokens` new tokens, at most max_new of one problem."""
+    att = RkvAttendParams(tokens, tokens if max_new is None else max_new, window, sinks, groups, 1, 1.0)
+    n = ctypes.c_size_t(0)
+    prm = shape.params()
+    s = load_library().rkv_attend_workspace_size(ctypes.byref(prm), ctypes.byref(att), ctypes.byref(n))
+    if s != RKV_OK:
+        raise RkvError(s, "rkv_attend_workspace_size")
+    return int(n.value)
+
+
+def make_attend_workspace(shape: Shape, tokens: int, max_new: Optional[int] = None, groups: int = 0, device="cuda") -> torch.Tensor:
+    """Scratch for calls with these sizes and any window."""
+    return torch.empty(rkv_attend_workspace_size(shape, tokens, max_new, groups) + 256, dtype=torch.uint8, device=device)
+
+
+def _attend(shape: Shape, q, k, v, starts, kv_len, group_starts, prefix_len, window, sinks, scale, max_new, ws, out, lse, want_lse, where):
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    _need_here(q, k, v, starts, kv_len, group_starts, prefix_len, ws, out, lse)
+    _check_kv(shape, k, "k")
+    _check_kv(shape, v, "v")
+    T = q.shape[0]
+    if not all(0 <= n <= _INT32_MAX for n in (window, sinks, 0 if max_new is None else max_new)):
+        raise ValueError("window, sinks and max_new must be in 0 .. 2^31 - 1")
+    _check_tokens(q, (T, shape.q_heads, shape.head_dim), "q")
+    _check_tokens(out, (T, shape.q_heads, shape.head_dim), "out")
+    if lse is not None and (tuple(lse.shape) != (T, shape.q_heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise ValueError(f"lse must be contiguous fp32 {(T, shape.q_heads)}")
+    _check_list(starts, shape.num_problems + 1, "starts")
+    _check_list(kv_len, shape.num_problems, "kv_len")
+    groups = 0
+    if group_starts is not None:
+        groups = prefix_len.shape[0]
+        _check_list(group_starts, groups + 1, "group_starts")
+        _check_list(prefix_len, groups, "prefix_len")
+    prm = shape.params(k, v)
+    att = RkvAttendParams(T, T if max_new is None else max_new, window, sinks, groups, _pages(shape, k, v),
+                          shape.head_dim ** -0.5 if scale is None else scale, _ptr(starts), _ptr(kv_len), _ptr(group_starts), _ptr(prefix_len),
+                          *_token_strides(q), *_token_strides(out))
+    lib = load_library()
+    if ws is None:
+        n = ctypes.c_size_t(0)
+        s = lib.rkv_attend_workspace_size(ctypes.byref(prm), ctypes.byref(att), ctypes.byref(n))
+        if s != RKV_OK:
+            raise RkvError(s, where)
+        ws = torch.empty(n.value + 256, dtype=torch.uint8, device=q.device)
+    base = ws.data_ptr()
+    aligned = (base + 255) & ~255
+    call = lib.rkv_attend if group_starts is None else lib.rkv_attend_shared
+    s = call(ctypes.byref(prm), ctypes.byref(att), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), aligned, ws.numel() - (aligned - base), _stream())
+    if s != RKV_OK:
+        raise RkvError(s, where)
+    return (out, lse) if lse is not None else out
+
+
+def rkv_attend(shape: Shape, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, kv_len: torch.Tensor,
+               window: int = 0, sinks: int = 0, scale: Optional[float] = None, max_new: Optional[int] = None,
+               ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """Causal attention of the new tokens q [T, q_heads, d] (ragged: starts) over their problems' caches, whose last rows are theirs: token
+    j of n sees the rows up to kv_len[p] - n + j, of those with a window only the last `window` and the first `sinks`.  Returns out,
+    or (out, lse) where the log of the softmax's sum is asked for.  scale: 1 / sqrt(d) unless given; max_new: most new tokens of a problem."""
+    return _attend(shape, q, k, v, starts, kv_len, None, None, window, sinks, scale, max_new, ws, out, lse, want_lse, "rkv_attend")
+
+
+def rkv_attend_shared(shape: Shape, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, kv_len: torch.Tensor,
+                      group_starts: torch.Tensor, prefix_len: torch.Tensor, window: int = 0, sinks: int = 0, scale: Optional[float] = None,
+                      max_new: Optional[int] = None, ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """rkv_attend for problems that share prompts: problems group_starts[g] .. group_starts[g + 1] - 1 hold the same values in their first
+    prefix_len[g] rows, which are read once for all of them, from the first one's cache."""
+    if group_starts is None or prefix_len is None:
+        raise ValueError("rkv_attend_shared needs group_starts and prefix_len")
+    return _attend(shape, q, k, v, starts, kv_len, group_starts, prefix_len, window, sinks, scale, max_new, ws, out, lse, want_lse,
+                   "rkv_attend_shared")

@@ -1,0 +1,221 @@
+"""include/rkv_attend.h: exported symbols, the parameter blocks' layout, and what the host refuses before anything is enqueued.  CPU only."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+from paper_2505_24133_amd import rkv
+
+FAKE = ctypes.c_void_p(0x1000)            # never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(rkv.LIB_PATH):
+        from paper_2505_24133_amd.build import build
+        build()
+    return rkv.load_library()
+
+
+def test_declared_symbols_are_exported_and_bound(lib, repo_root):
+    text = open(os.path.join(repo_root, "include", "rkv_attend.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = sorted(set(re.findall(r"\b(rkv_[a-z_]+)\s*\(", text)))
+    assert names == ["rkv_attend", "rkv_attend_shared", "rkv_attend_workspace_size", "rkv_cache_append_rotary"]
+    import paper_2505_24133_amd as package
+    for n in names:
+        assert hasattr(lib, n) and hasattr(rkv, n) and getattr(package, n) is getattr(rkv, n)
+
+
+@pytest.mark.parametrize("struct,mirror", [("rkv_rotary_params", rkv.RkvRotaryParams), ("rkv_attend_params", rkv.RkvAttendParams)])
+def test_layout_matches_header(repo_root, tmp_path, struct, mirror):
+    names = [f[0] for f in mirror._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "rkv_attend.h"\nint main(void) {\n'
+                   f'  printf("%zu\\n", sizeof({struct}));\n'
+                   + "".join(f'  printf("%zu\\n", offsetof({struct}, {n}));\n' for n in names) + "  return 0;\n}\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-I", os.path.join(repo_root, "include"), "-o", str(exe), str(src)], check=True)
+    out = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert out[0] == ctypes.sizeof(mirror)
+    assert out[1:] == [getattr(mirror, n).offset for n in names]
+
+
+def shape(**kw):
+    base = dict(num_problems=2, kv_heads=8, q_heads=32, n_tokens=1152, budget=1024)
+    base.update(kw)
+    return rkv.Shape(**base)
+
+
+def block(s, **kw):
+    p = s.params()
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def att(**kw):
+    base = dict(tokens=2, max_new=1, scale=0.1, starts=0x1000, kv_len=0x1000)
+    base.update(kw)
+    return rkv.RkvAttendParams(**base)
+
+
+def size(lib, p, a):
+    n = ctypes.c_size_t(0)
+    return lib.rkv_attend_workspace_size(ctypes.byref(p) if p else None, ctypes.byref(a) if a else None, ctypes.byref(n)), n.value
+
+
+def test_attend_sizes_and_refusals(lib):
+    ok = block(shape())
+    st, n = size(lib, ok, att())
+    assert st == rkv.RKV_OK and n % 256 == 0
+    assert size(lib, None, att())[0] == rkv.RKV_ERR_NULL and size(lib, ok, None)[0] == rkv.RKV_ERR_NULL
+    assert lib.rkv_attend_workspace_size(ctypes.byref(ok), ctypes.byref(att()), None) == rkv.RKV_ERR_NULL
+    # nothing to do needs nothing
+    assert size(lib, block(shape(num_problems=0)), att(tokens=0)) == (rkv.RKV_OK, 0)
+    assert size(lib, ok, att(tokens=0, max_new=0)) == (rkv.RKV_OK, 0)
+    # what the compression step asks beyond the caches is not asked
+    assert size(lib, block(shape(q_heads=8 * 9)), att())[0] == rkv.RKV_OK
+    assert size(lib, block(shape(n_tokens=1 << 20, budget=1 << 21)), att())[0] == rkv.RKV_OK
+    for bad in (dict(num_problems=-1), dict(kv_heads=0), dict(q_heads=30), dict(n_tokens=0)):
+        assert size(lib, block(ok_shape(), **bad), att())[0] == rkv.RKV_ERR_SHAPE, bad
+    for bad in (dict(head_dim=64), dict(n_tokens=(1 << 24) + 1), dict(kv_heads=1, q_heads=5000)):
+        assert size(lib, block(ok_shape(), **bad), att())[0] == rkv.RKV_ERR_UNSUPPORTED, bad
+    for bad in (dict(tokens=-1), dict(max_new=0), dict(max_new=3), dict(groups=-1), dict(groups=3)):
+        assert size(lib, ok, att(**bad))[0] == rkv.RKV_ERR_SHAPE, bad
+    for bad in (dict(window=-1), dict(sinks=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
+        assert size(lib, ok, att(**bad))[0] == rkv.RKV_ERR_PARAM, bad
+    assert size(lib, ok, att(tokens=(1 << 24) + 1))[0] == rkv.RKV_ERR_UNSUPPORTED
+    for bad in (dict(q_stride_token=100, q_stride_head=128), dict(q_stride_token=4096, q_stride_head=-128), dict(o_stride_token=0, o_stride_head=128),
+                dict(o_stride_token=4096, o_stride_head=0), dict(q_stride_token=1 << 41, q_stride_head=128)):
+        assert size(lib, ok, att(**bad))[0] == rkv.RKV_ERR_SHAPE, bad
+    for bad in (dict(k_stride_token=100, k_stride_head=8, k_stride_problem=8), dict(v_stride_token=128, v_stride_head=0, v_stride_problem=8),
+                dict(k_stride_token=128, k_stride_head=8, k_stride_problem=0), dict(v_stride_token=40000, v_stride_head=8, v_stride_problem=8)):
+        assert size(lib, block(shape(), **bad), att())[0] == rkv.RKV_ERR_SHAPE, bad
+
+
+def ok_shape():
+    return shape()
+
+
+def paged(**kw):
+    base = dict(page_size=16, table_stride=72, block_table=0x1000, k_stride_page=8 * 16 * 128, v_stride_page=8 * 16 * 128,
+                k_stride_head=16 * 128, v_stride_head=16 * 128, k_stride_token=128, v_stride_token=128)
+    base.update(kw)
+    return block(shape(), **base)
+
+
+def test_paged_caches(lib):
+    assert size(lib, paged(), att(num_pages=5))[0] == rkv.RKV_OK
+    assert size(lib, paged(), att(num_pages=0))[0] == rkv.RKV_ERR_SHAPE
+    assert size(lib, paged(page_size=24), att(num_pages=5))[0] == rkv.RKV_ERR_UNSUPPORTED
+    assert size(lib, paged(block_table=None), att(num_pages=5))[0] == rkv.RKV_ERR_NULL
+    assert size(lib, paged(table_stride=71), att(num_pages=5))[0] == rkv.RKV_ERR_SHAPE
+    assert size(lib, paged(k_stride_page=0), att(num_pages=5))[0] == rkv.RKV_ERR_SHAPE
+    assert size(lib, paged(v_stride_token=64), att(num_pages=5))[0] == rkv.RKV_ERR_SHAPE
+    assert size(lib, paged(k_stride_head=0), att(num_pages=5))[0] == rkv.RKV_ERR_SHAPE
+
+
+def test_workspace_grows_with_the_parts_only(lib):
+    """A batch that fills the chip by itself needs none; one sequence over a long cache does; a window never needs more."""
+    assert size(lib, block(shape(num_problems=64)), att(tokens=64))[1] == 0
+    long = size(lib, block(shape(num_problems=1, n_tokens=32768)), att(tokens=1))[1]
+    assert long > 0
+    for window in (1, 100, 4096, 2 ** 31 - 1):
+        assert size(lib, block(shape(num_problems=1, n_tokens=32768)), att(tokens=1, window=window, sinks=2 ** 31 - 1))[1] <= long
+    # never more than some hundred MB, whatever is asked for without a shared prefix
+    for P in (1, 2, 64):
+        for T in (1, 64, 1000, 16000):
+            for G in (1, 4, 64, 128):
+                p = block(shape(num_problems=P, n_tokens=32768, kv_heads=8, q_heads=8 * G))
+                st, n = size(lib, p, att(tokens=max(T, P), max_new=max(1, T // P)))
+                assert st == rkv.RKV_OK and n < 400e6, (P, T, G, n)
+
+
+def test_attend_refuses_before_anything_is_enqueued(lib):
+    p = block(shape())
+
+    def call(a, q=FAKE, k=FAKE, v=FAKE, out=FAKE, ws=FAKE, n=1 << 40, shared=False, prm=p):
+        f = lib.rkv_attend_shared if shared else lib.rkv_attend
+        return f(ctypes.byref(prm) if prm else None, ctypes.byref(a) if a else None, q, k, v, out, None, ws, n, None)
+
+    for missing in ("q", "k", "v", "out"):
+        assert call(att(), **{missing: None}) == rkv.RKV_ERR_NULL
+        assert call(att(), **{missing: ctypes.c_void_p(0x1008)}) == rkv.RKV_ERR_SHAPE
+    assert call(att(starts=None)) == rkv.RKV_ERR_NULL and call(att(kv_len=None)) == rkv.RKV_ERR_NULL
+    assert call(att(), prm=None) == rkv.RKV_ERR_NULL and call(None) == rkv.RKV_ERR_NULL
+    assert call(att(groups=1)) == rkv.RKV_ERR_SHAPE                        # groups are rkv_attend_shared's
+    assert call(att(groups=1), shared=True) == rkv.RKV_ERR_NULL            # and come with their lists
+    assert call(att(groups=1, group_starts=0x1000), shared=True) == rkv.RKV_ERR_NULL
+    need = size(lib, p, att())[1]
+    assert need > 0
+    assert call(att(), ws=None) == rkv.RKV_ERR_WORKSPACE
+    assert call(att(), ws=ctypes.c_void_p(0x1010)) == rkv.RKV_ERR_WORKSPACE
+    assert call(att(), n=need - 1) == rkv.RKV_ERR_WORKSPACE
+    assert call(att(tokens=0, max_new=0), q=None, k=None, v=None, out=None, ws=None, n=0) == rkv.RKV_OK
+    assert call(att(scale=0.0)) == rkv.RKV_ERR_PARAM
+
+
+def test_append_refuses_before_anything_is_enqueued(lib):
+    p = block(shape())
+
+    def rot(**kw):
+        base = dict(tokens=2, rotary_dim=128, table_rows=10, cos=0x1000, sin=0x1000, starts=0x1000, held=0x1000, seen=0x1000)
+        base.update(kw)
+        return rkv.RkvRotaryParams(**base)
+
+    def call(r, args=(FAKE,) * 7, prm=p):
+        return lib.rkv_cache_append_rotary(ctypes.byref(prm) if prm else None, ctypes.byref(r) if r else None, *args, None)
+
+    assert call(None) == rkv.RKV_ERR_NULL and call(rot(), prm=None) == rkv.RKV_ERR_NULL
+    for i in range(7):
+        if i != 2:                                                         # the query cache is optional
+            assert call(rot(), (FAKE,) * i + (None,) + (FAKE,) * (6 - i)) == rkv.RKV_ERR_NULL, i
+        assert call(rot(), (FAKE,) * i + (ctypes.c_void_p(0x1004),) + (FAKE,) * (6 - i)) == rkv.RKV_ERR_SHAPE, i
+    for name in ("cos", "sin", "starts", "held", "seen"):
+        assert call(rot(**{name: None})) == rkv.RKV_ERR_NULL
+    for name in ("cos", "sin"):
+        assert call(rot(**{name: 0x1004})) == rkv.RKV_ERR_SHAPE
+    assert call(rot(tokens=-1)) == rkv.RKV_ERR_SHAPE and call(rot(table_rows=0)) == rkv.RKV_ERR_SHAPE
+    for r in (0, 8, 24, 144, -16):
+        assert call(rot(rotary_dim=r)) == rkv.RKV_ERR_UNSUPPORTED
+    assert call(rot(interleaved=2)) == rkv.RKV_ERR_PARAM
+    assert call(rot(tokens=1 << 24)) == rkv.RKV_ERR_UNSUPPORTED
+    for name in ("k", "v", "q", "o"):
+        assert call(rot(**{f"{name}_stride_token": 100, f"{name}_stride_head": 128})) == rkv.RKV_ERR_SHAPE
+        assert call(rot(**{f"{name}_stride_token": 4096, f"{name}_stride_head": 0})) == rkv.RKV_ERR_SHAPE
+    assert call(rot(), prm=block(shape(), alpha=0)) == rkv.RKV_ERR_SHAPE
+    assert call(rot(), prm=block(shape(), q_stride_token=64, q_stride_head=128, q_stride_problem=128)) == rkv.RKV_ERR_SHAPE
+    assert call(rot(), prm=paged()) == rkv.RKV_ERR_SHAPE                   # a pool without pages
+    assert call(rot(tokens=0), (None,) * 7) == rkv.RKV_OK
+
+
+def test_binding_refuses(lib):
+    s = shape(num_problems=1, kv_heads=1, q_heads=4, n_tokens=64, budget=32)
+    kv = torch.zeros((1, 1, 64, 128), dtype=torch.bfloat16)
+    q = torch.zeros((1, 4, 128), dtype=torch.bfloat16)
+    one = torch.zeros(1, dtype=torch.int32)
+    two = torch.zeros(2, dtype=torch.int32)
+    table = torch.zeros((10, 64))
+    with pytest.raises(RuntimeError, match="no CPU path"):
+        rkv.rkv_attend(s, q, kv, kv, two, one)
+    with pytest.raises(RuntimeError, match="no CPU path"):
+        rkv.rkv_attend_shared(s, q, kv, kv, two, one, two, one)
+    with pytest.raises(ValueError, match="needs group_starts"):
+        rkv.rkv_attend_shared(s, q, kv, kv, two, one, None, None)
+    with pytest.raises(RuntimeError, match="no CPU path"):
+        rkv.rkv_cache_append_rotary(s, kv, kv, None, q[:, :1], q[:, :1], q, table, table, two, one, one)
+    with pytest.raises(rkv.RkvError, match="status -2"):
+        rkv.rkv_attend_workspace_size(s, 5, max_new=6)
+
+
+def test_rotary_tables_at_far_positions():
+    """The angles of far positions are formed in 64 bits: the last of a million rows is as exact as the first."""
+    cos, sin = rkv.rotary_tables(1000001, 16, 500000.0, device="cpu")
+    import math
+    for i in range(8):
+        angle = 1000000 * 500000.0 ** (-2 * i / 16)
+        assert abs(cos[-1, i].item() - math.cos(angle)) < 1e-7 and abs(sin[-1, i].item() - math.sin(angle)) < 1e-7

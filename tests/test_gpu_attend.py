@@ -1,0 +1,247 @@
+"""Attention over contiguous and paged caches against float64: single tokens, drafts, prompts and mixtures of them, windows and sinks, odd
+lengths, rows that see nothing, what must not be seen, strides, streams, graphs and workspaces."""
+import math
+
+import pytest
+import torch
+
+from attend_reference import Batch, attend64, check, int32
+from paper_2505_24133_amd import rkv
+
+pytestmark = pytest.mark.gpu
+
+
+def run(b, window=0, sinks=0, **kw):
+    kw.setdefault("max_new", max(max(b.new), 1))
+    return rkv.rkv_attend(b.shape, b.q, b.k, b.v, b.starts, b.kv_len, window=window, sinks=sinks, want_lse=True, **kw)
+
+
+def both(b, window=0, sinks=0, scale=None, where=""):
+    check(run(b, window, sinks, scale=scale), attend64(b, window, sinks, scale), where)
+
+
+@pytest.mark.parametrize("H,G,new,lens,page,strided", [
+    pytest.param(1, 1, [1], [1], 0, False, id="one token over itself"),
+    pytest.param(2, 4, [1, 1, 1], [2, 31, 32], 0, False, id="lengths around a tile"),
+    pytest.param(2, 4, [1, 1, 1, 1], [33, 63, 64, 65], 16, False, id="paged, lengths around a tile and a page"),
+    pytest.param(8, 4, [1], [1152], 0, True, id="a full cache, tokens outside heads in memory"),
+    pytest.param(8, 4, [1], [1152], 16, False, id="a full paged cache"),
+    pytest.param(3, 5, [1, 3, 2, 0, 1], [700, 5, 129, 40, 1000], 32, False, id="drafts of different lengths, one problem without"),
+    pytest.param(2, 7, [5, 1], [333, 87], 64, False, id="35 rows of queries"),
+    pytest.param(1, 16, [2], [301], 0, False, id="32 rows of queries"),
+    pytest.param(1, 64, [1], [301], 128, False, id="64 query heads a KV head"),
+    pytest.param(1, 71, [1], [301], 0, False, id="71 query heads a KV head"),
+    pytest.param(2, 4, [1], [32768], 16, False, id="the longest cache of the step"),
+    pytest.param(1, 1, [1], [70001], 0, False, id="a longer one"),
+    pytest.param(1, 4, [1] * 300, [17 + i for i in range(300)], 16, False, id="300 problems"),
+])
+def test_few_rows(H, G, new, lens, page, strided):
+    print(f"[gpu-case] attend few H={H} G={G} P={len(new)} page={page}", flush=True)
+    both(Batch(H, G, new, lens, page=page, strided=strided, seed=len(lens) + lens[0]))
+
+
+@pytest.mark.parametrize("H,G,new,lens,page,strided", [
+    pytest.param(2, 1, [65], [65], 0, False, id="65 tokens, one query head"),
+    pytest.param(2, 4, [128], [128], 0, False, id="whole tiles"),
+    pytest.param(1, 4, [129], [129], 16, False, id="one token more than a tile"),
+    pytest.param(3, 5, [63, 64, 65], [63, 64, 65], 32, False, id="three prompts around a step"),
+    pytest.param(2, 4, [200, 1, 0, 77, 16, 17], [200, 900, 50, 500, 16, 600], 16, False, id="prompts, chunks, single tokens"),
+    pytest.param(4, 7, [511], [2100], 64, False, id="a chunk behind a cache, split over workgroups"),
+    pytest.param(1, 8, [1000], [1000], 0, True, id="a prompt, tokens outside heads in memory"),
+    pytest.param(2, 3, [700] * 70 + [1] * 30, [700] * 70 + [300] * 30, 128, False, id="100 problems: more than one look at the list"),
+    pytest.param(1, 100, [3, 1], [40, 90], 0, False, id="100 query heads a KV head"),
+])
+def test_many_rows(H, G, new, lens, page, strided):
+    print(f"[gpu-case] attend many H={H} G={G} P={len(new)} page={page}", flush=True)
+    both(Batch(H, G, new, lens, page=page, strided=strided, seed=len(lens) + lens[0]))
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 4), (64, 0), (64, 70), (100, 3), (257, 64), (2000, 4), (2 ** 31 - 1, 5)])
+@pytest.mark.parametrize("page", [0, 16])
+def test_window_and_sinks(window, sinks, page):
+    print(f"[gpu-case] attend window={window} sinks={sinks} page={page}", flush=True)
+    both(Batch(2, 4, [1, 1, 1, 3], [1, 40, 1300, 515], page=page, seed=1), window, sinks, where="few rows")
+    both(Batch(1, 4, [300, 64, 1, 100], [300, 700, 900, 100], page=page, seed=2), window, sinks, where="many rows")
+    both(Batch(1, 5, [130], [1500], page=page, seed=3), window, sinks, where="a chunk, split")
+
+
+def test_rows_that_see_nothing():
+    """Fewer rows than new tokens: the first ones see nothing; so does everyone over an empty cache."""
+    for G, new, lens in ((4, [3, 2, 1], [1, 0, 7]), (4, [90, 40], [33, 0]), (2, [100], [0])):
+        b = Batch(2, G, new, lens, N=50, seed=5)
+        both(b)
+        both(b, window=3, sinks=2)
+
+
+@pytest.mark.parametrize("fill", [math.nan, math.inf, -3e38])
+@pytest.mark.parametrize("page", [0, 16])
+def test_what_lies_behind_the_rows_is_not_seen(fill, page):
+    b = Batch(2, 4, [1, 2, 1], [1, 45, 600], N=777, page=page, fill=fill, seed=6)
+    both(b)
+    both(b, window=20, sinks=2)
+    b = Batch(2, 4, [45, 200], [45, 333], N=400, page=page, fill=fill, seed=7)
+    both(b)
+    both(b, window=30, sinks=3)
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("new,lens", [([200], [200]), ([100], [333]), ([4], [77]), ([16], [200])])
+def test_what_other_tokens_see_is_not_seen(value, new, lens):
+    """A value or a key that is not finite in the row of one token: the tokens before it are as if it were not there."""
+    for which in ("k", "v"):
+        b = Batch(2, 4, new, lens, seed=8)
+        at = lens[0] - 2                                     # the row of the last token but one
+        (b.rows_k if which == "k" else b.rows_v)[0, :, at, 5] = value
+        b.store()
+        out, lse = run(b)
+        ref = attend64(b)
+        first = new[0] - 2
+        check((out[:first], lse[:first]), tuple(t[:first] for t in ref), which)
+        if which == "v":
+            hit = out[first:, :, 5]
+            assert (torch.isnan(hit) if math.isnan(value) else hit == value).all()
+            rest = [c for c in range(128) if c != 5]
+            check((out[first:][..., rest], lse[first:]), (ref[0][first:][..., rest], ref[1][first:], ref[2][first:][..., rest], ref[3][first:]))
+        # behind a window that has passed the row, nothing of it is left
+        b = Batch(2, 4, new, lens, seed=9)
+        (b.rows_k if which == "k" else b.rows_v)[0, :, 4, 5] = value
+        b.store()
+        window = max(1, lens[0] - new[0] - 5) if lens[0] > new[0] + 5 else 3
+        first = max(0, 5 + window - (lens[0] - new[0]))      # tokens from here on do not see row 4
+        out, lse = run(b, window, 2)
+        check((out[first:], lse[first:]), tuple(t[first:] for t in attend64(b, window, 2)), which)
+
+
+def test_large_and_small_scores():
+    """Scores far apart (the maximum moves late, early and not at all), all equal, and all very low."""
+    for new, lens in (([1], [500]), ([130], [500])):
+        for how in ("rising", "falling", "equal", "low"):
+            b = Batch(1, 4, new, lens, seed=10)
+            q0 = torch.randn(128, device="cuda", generator=b.gen).bfloat16()
+            ramp = {"rising": torch.linspace(-3, 3, lens[0]), "falling": torch.linspace(3, -3, lens[0]), "equal": torch.zeros(lens[0]),
+                    "low": torch.full((lens[0],), -40.0)}[how].cuda()
+            b.q[:] = q0
+            b.rows_k[0, 0] = (ramp[:, None] * q0.float()[None]).bfloat16()
+            b.store()
+            both(b, where=how)
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.01, 1e-30])
+def test_scale(scale):
+    both(Batch(2, 4, [1, 2], [100, 200], seed=11), scale=scale)
+    both(Batch(2, 4, [100], [200], seed=11), scale=scale)
+
+
+def test_strided_queries_and_outputs_and_rows_behind_the_batch():
+    """Queries and outputs inside wider rows, and tokens behind the last problem, which stay as they are."""
+    for new, lens in (([2, 1], [50, 300]), ([90, 3], [200, 300])):
+        b = Batch(2, 3, new, lens, seed=12, extra_tokens=5)
+        wide = torch.full((b.T, 10, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        wide[:, 1:7] = b.q
+        room = torch.full((b.T, 9, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((b.T, 6), 4.0, device="cuda")
+        rkv.rkv_attend(b.shape, wide[:, 1:7], b.k, b.v, b.starts, b.kv_len, max_new=max(new), out=room[:, 2:8], lse=lse)
+        n = sum(new)
+        check((room[:n, 2:8], lse[:n]), tuple(t[:n] for t in attend64(b)))
+        assert (room[n:] == 9).all() and (room[:, :2] == 9).all() and (room[:, 8:] == 9).all() and (lse[n:] == 4).all()
+
+
+def test_any_bound_on_the_new_tokens_gives_the_same_up_to_rounding():
+    b = Batch(2, 4, [1, 2, 1], [50, 300, 1000], seed=13, page=16)
+    want = attend64(b)
+    for max_new in (2, 3, 4):
+        check(run(b, max_new=max_new), want)
+    check(rkv.rkv_attend(b.shape, b.q, b.k, b.v, b.starts, b.kv_len, want_lse=True), want)
+
+
+def test_a_query_has_the_same_bits_in_any_company():
+    """The same call twice gives the same bits, and so does another workspace full of other values."""
+    for new, lens in (([1, 2], [700, 9000]), ([100], [5000])):
+        b = Batch(2, 4, new, lens, seed=14)
+        ws = rkv.make_attend_workspace(b.shape, b.T, max(new))
+        first = run(b, ws=ws.fill_(0xff))
+        again = run(b, ws=ws.fill_(0x7f))
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
+def test_lists_outside_their_ranges_read_nothing_outside():
+    """Lengths past the cache, below zero, pages that are not in the pool: nothing is read out of bounds; the rest is as it should be."""
+    b = Batch(2, 4, [1, 1, 1], [40, 64, 64], N=64, page=16, seed=15)
+    b.kv_len.copy_(int32([40, 1000, -5]))
+    b.table[0, 3] = 10 ** 6                                 # behind the rows of problem 0
+    out, lse = run(b)
+    b.lens = [40, 64, 0]
+    check((out, lse), attend64(b))
+    b.table[0, 0] = -7
+    b.table[1, 2] = 2 ** 31 - 1
+    out, _ = run(b)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out.float()).all()
+
+
+def test_other_stream_and_graph():
+    b = Batch(2, 4, [1, 1], [300, 2000], seed=16, page=16)
+    ws = rkv.make_attend_workspace(b.shape, b.T, 1)
+    out, lse = run(b, ws=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = run(b, ws=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out, other[0]) and torch.equal(lse, other[1])
+    # a graph follows its inputs: lengths, queries and rows change between replays
+    held = torch.empty_like(out), torch.empty_like(lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(b, ws=ws, out=held[0], lse=held[1])
+    for lens in ([300, 2000], [1, 77], [299, 1500]):
+        b.lens = lens
+        b.kv_len.copy_(int32(lens))
+        b.q.normal_(generator=b.gen)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(held, attend64(b))
+        eager = run(b)
+        assert torch.equal(held[0], eager[0]) and torch.equal(held[1], eager[1])
+
+
+def test_two_graphs_with_one_workspace():
+    """Two captured calls that share a workspace, replayed one after the other in any order."""
+    a, b = Batch(2, 4, [1], [3000], seed=17), Batch(2, 4, [70], [500], seed=18)
+    ws = torch.empty(max(rkv.make_attend_workspace(x.shape, x.T, x.new[0]).numel() for x in (a, b)), dtype=torch.uint8, device="cuda")
+    want = [run(x) for x in (a, b)]
+    got, graphs = [], []
+    for x in (a, b):
+        got.append((torch.empty_like(x.q), torch.empty(x.q.shape[:2], device="cuda")))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(x, ws=ws, out=got[-1][0], lse=got[-1][1])
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1)):
+        for i in order:
+            got[i][0].zero_()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got[i][0], want[i][0]) and torch.equal(got[i][1], want[i][1])
+
+
+def test_cache_past_32_bits_of_offset():
+    """Rows whose offset passes 2^31 elements and 2^32 bytes."""
+    H, N = 1, 4096
+    k = torch.empty((5000, N, 128), dtype=torch.bfloat16, device="cuda")        # 2.6e9 elements
+    b = Batch(1, 4, [1, 1], [4096, 700], seed=19)
+    big = k.as_strided((2, H, N, 128), (4998 * N * 128, N * 128, 128, 1))
+    big.copy_(b.rows_k)
+    shape = rkv.Shape(num_problems=2, kv_heads=1, q_heads=4, n_tokens=N, budget=N - 1)
+    got = rkv.rkv_attend(shape, b.q, big, b.v, b.starts, b.kv_len, max_new=1, want_lse=True)
+    check(got, attend64(b))
+    pool = k.view(5000 * N // 16, 1, 16, 128)
+    table = torch.empty((2, N // 16), dtype=torch.int32, device="cuda")
+    table[0] = pool.shape[0] - 1 - torch.arange(N // 16, device="cuda")
+    table[1] = torch.arange(N // 16, device="cuda")
+    for p in range(2):
+        pool[table[p].long()] = b.rows_k[p].reshape(1, N // 16, 16, 128).transpose(0, 1)
+    values = pool.clone()
+    for p in range(2):
+        values[table[p].long()] = b.rows_v[p].reshape(1, N // 16, 16, 128).transpose(0, 1)
+    shape.page_size, shape.block_table = 16, table
+    check(rkv.rkv_attend(shape, b.q, pool, values, b.starts, b.kv_len, max_new=1, want_lse=True), attend64(b))
