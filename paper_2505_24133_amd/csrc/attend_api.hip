@@ -13,7 +13,10 @@ namespace {
 
 constexpr int kMaxTokens = 1 << 24;
 constexpr int64_t kMaxBlocks = 1 << 23;
-constexpr int kSlots = 512;                 // workgroups that the chip's 256 compute units hold of the kernel for many rows
+constexpr int64_t kSlots = 512;             // workgroups of the many-rows kernel that the chip's 256 compute units hold
+constexpr int64_t kSmallSlots = 512;        // and of the few-rows kernel
+constexpr int64_t kSmallShare = 64;         // fewest rows of one of its workgroups
+constexpr int64_t kMaxSplits = 128;         // (the join takes 256 parts)
 
 bool row_stride(int64_t s) { return s >= kHeadDim && s <= 32768 && s % 8 == 0; }
 bool wide_stride(int64_t s, bool several) { return s >= 0 && s % 8 == 0 && (s > 0 || !several); }
@@ -64,8 +67,26 @@ struct AttendPlan {
   size_t off_small_o, off_small_ml, off_tile_o, off_tile_ml, off_prefix_o, off_prefix_ml, total;
 };
 
-int split_over(int64_t blocks, int64_t slots, int64_t most) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>((slots + blocks - 1) / std::max<int64_t>(blocks, 1), most));
+// Into how many workgroups the rows of a few-rows unit are dealt: as many as the chip takes at once, then more where a unit still has a
+// thousand rows for each, so that units of different lengths even out.
+int small_splits(int64_t units, int64_t reach) {
+  const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + kSmallShare - 1) / kSmallShare);
+  const int64_t even = std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
+}
+
+// Likewise for the tiles of the many-rows kernel where they do not fill the chip: rounds of workgroups times steps of each, two of
+// them for its start.
+int tile_splits(int64_t tiles, int64_t reach) {
+  if (tiles >= kSlots) return 1;
+  const int64_t steps = (reach + 31) / 32;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 32 && (s == 1 || s * 4 <= steps); ++s) {
+    const double cost = (double)((tiles * s + kSlots - 1) / kSlots) * (double)((steps + s - 1) / s + 2);
+    if (s == 1 || cost < 0.98 * least) { best = s; least = cost; }
+  }
+  return best;
 }
 
 rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool shared, AttendPlan* pl) {
@@ -99,13 +120,12 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   const bool small = !large || (c.P > 1 && c.G <= kSmallRows);
   // rows that a query may see, at most
   const int64_t reach = t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + t.max_new) : c.N;
-  // A unit's rows are dealt to several workgroups where there are fewer units than the chip takes at once (256 and 512)
   if (small) {
     a.small_rows = large || most_rows > 32 ? 64 : (most_rows > 16 ? 32 : 16);
-    a.small_splits = split_over((int64_t)c.P * c.H, 256, (reach + 127) / 128);
+    a.small_splits = small_splits((int64_t)c.P * c.H, reach);
   }
-  if (large) a.tile_splits = split_over(attend_tile_bound(t.tokens, c.G, c.P) * c.H, kSlots, std::min<int64_t>((reach + 255) / 256, 32));
-  if (t.groups > 0) a.prefix_splits = split_over(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, kSlots, std::min<int64_t>((reach + 255) / 256, 32));
+  if (large) a.tile_splits = tile_splits(attend_tile_bound(t.tokens, c.G, c.P) * c.H, reach);
+  if (t.groups > 0) a.prefix_splits = tile_splits(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, reach);
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
       (int64_t)t.tokens * ((c.H * c.G + 7) / 8) > kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)

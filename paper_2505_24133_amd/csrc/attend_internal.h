@@ -82,16 +82,17 @@ __device__ __forceinline__ Sight sight(const AttendArgs& a, int r) {
   return Sight{a.window > 0 ? max(r - a.window + 1, 0) : 0, max(r + 1, 0)};
 }
 
-// The rows of [base, lim) that a block of queries reads, in tiles of TK: those before `sinks` and those from the lowest lo on.
+// The rows of [base, lim) that a block of queries reads, in tiles of TK that start at multiples of 16 (16 rows from there on lie in one
+// page): those before `sinks` and those from the lowest lo on.  No row lies in both.
 template <int TK>
 struct Span {
   int start_a, end_a, tiles_a, start_b, end_b, tiles;
   __device__ __forceinline__ Span(int base, int lim, int lo_min, int hi_max, int sinks) {
     end_b = min(hi_max, lim);
-    start_b = max(base, lo_min);
-    start_a = base;
+    start_b = max(base, lo_min) & ~15;
+    start_a = base & ~15;
     end_a = min(min(sinks, lim), hi_max);
-    if (end_a >= start_b) { start_b = base; end_a = base; }
+    if (end_a >= start_b) { start_b = start_a; end_a = start_a; }
     tiles_a = end_a > start_a ? (end_a - start_a + TK - 1) / TK : 0;
     tiles = tiles_a + (end_b > start_b ? (end_b - start_b + TK - 1) / TK : 0);
   }
@@ -100,69 +101,104 @@ struct Span {
 };
 
 // --------------------------------------------------------------------------------------------- where rows lie
-// Rows of one problem and head.  Paged: the ids of 64 consecutive pages lie in the lanes of the wave (1024 rows and more), and a
-// row's page is fetched from its lane; reload() is called with wave-uniform rows before rows are looked up.
-template <bool PAGED>
+// Rows of one problem and head, copied to LDS 16 at a time (four copies of four rows, 16 bytes a lane), keys and values.  The address of
+// the 16 rows is the same in all lanes, a lane adds its offset among four rows.  Paged: the ids of 64 consecutive pages lie in the
+// lanes of the wave (1024 rows and more); reload() is called with wave-uniform rows before rows are copied.
+//
+// Places in LDS of 16-byte piece `chunk` of row `row`: keys are read 16 rows at one chunk (the four low bits of the row spread
+// them over all banks), values four rows at two neighbouring chunks, transposed (pairs of chunks are spread by three bits of the row).
+__device__ __forceinline__ int key_chunk(int row, int chunk) { return chunk ^ (row & 15); }
+__device__ __forceinline__ int value_chunk(int row, int chunk) { return chunk ^ ((row & 7) << 1); }
+
+template <bool PAGED, int FOURS>
 struct Rows {
-  const uint16_t* k;
-  const uint16_t* v;
+  const unsigned char* k;
+  const unsigned char* v;
   const int32_t* table;
-  int shift, pages, num_pages, first, ids;
-  int64_t kst, vst, kspage, vspage;
-  __device__ __forceinline__ Rows(const AttendArgs& a, int p, int h) {
-    k = a.k + h * a.kl.sh;
-    v = a.v + h * a.vl.sh;
-    kst = a.kl.st; vst = a.vl.st;
+  int N, shift, pages, num_pages, first, ids;
+  uint32_t kst, vst;             // bytes
+  int64_t kspage, vspage;        // bytes
+  uint32_t koff[FOURS], voff[FOURS];     // of this lane: its row of four, and the chunk that belongs at its place
+  int c0;
+  // This wave copies FOURS times four rows of 16, from row 4 c0 on.
+  __device__ __forceinline__ Rows(const AttendArgs& a, int p, int h, int c0) : c0(c0) {
+    k = reinterpret_cast<const unsigned char*>(a.k + h * a.kl.sh);
+    v = reinterpret_cast<const unsigned char*>(a.v + h * a.vl.sh);
+    N = a.N;
+    kst = (uint32_t)a.kl.st * 2; vst = (uint32_t)a.vl.st * 2;
     if constexpr (PAGED) {
       shift = a.kl.page_shift;
       pages = (a.N + (1 << shift) - 1) >> shift;
       num_pages = a.num_pages;
       table = a.kl.table + (int64_t)p * a.kl.table_stride;
-      kspage = a.kl.spage; vspage = a.vl.spage;
+      kspage = a.kl.spage * 2; vspage = a.vl.spage * 2;
       first = -64;
       ids = 0;
     } else {
-      k += p * a.kl.sp;
-      v += p * a.vl.sp;
+      k += p * a.kl.sp * 2;
+      v += p * a.vl.sp * 2;
     }
+#pragma unroll
+    for (int c = 0; c < FOURS; ++c) offsets(c, 15, &koff[c], &voff[c]);
+  }
+  // Offsets of copy c of this lane; rows past `last` of the 16 are that one.
+  __device__ __forceinline__ void offsets(int c, int last, uint32_t* ko, uint32_t* vo) const {
+    const int lane = threadIdx.x & 63, row = 4 * (c0 + c) + (lane >> 4), from = min(row, last);
+    *ko = from * kst + (key_chunk(row, lane & 15) << 4);
+    *vo = from * vst + (value_chunk(row, lane & 15) << 4);
   }
   __device__ __forceinline__ void reload(int row_lo, int row_hi) {
     if constexpr (PAGED) {
-      const int lo = row_lo >> shift, hi = row_hi >> shift;
+      const int lo = row_lo >> shift, hi = min(row_hi, N - 1) >> shift;
       if (lo < first || hi >= first + 64) {
         first = lo;
         ids = clampi(table[min(lo + (int)(threadIdx.x & 63), pages - 1)], 0, num_pages - 1);
       }
     }
   }
-  // Addresses of 16-byte piece ck of row's key and piece cv of its value.
-  __device__ __forceinline__ void find(int row, int ck, int cv, const uint16_t** kp, const uint16_t** vp) const {
+  // Where 16 rows lie that start at a multiple of 16.  Rows past the cache's last one are the last 16 again.
+  struct Place { int at, page; };
+  __device__ __forceinline__ Place place(int row16) const {
+    const int at = __builtin_amdgcn_readfirstlane(min(row16, (N - 1) & ~15));
+    if constexpr (PAGED) return Place{at, __builtin_amdgcn_readlane(ids, ((at >> shift) - first) & 63)};
+    return Place{at, 0};
+  }
+  // Its keys and values to LDS.  Past the end of a contiguous cache a lane pulls its row back to the last one, in a page there is room:
+  // the caller hides what is past the end.
+  __device__ __forceinline__ void copy(Place w, uint32_t k_to, uint32_t v_to) const {
+    const unsigned char *kb, *vb;
     if constexpr (PAGED) {
-      const int page = __builtin_amdgcn_ds_bpermute(((row >> shift) - first) << 2, ids);
-      const int slot = row & ((1 << shift) - 1);
-      *kp = k + page * kspage + slot * kst + ck * 8;
-      *vp = v + page * vspage + slot * vst + cv * 8;
+      const uint32_t slot = w.at & ((1 << shift) - 1);
+      kb = k + w.page * kspage + slot * kst;
+      vb = v + w.page * vspage + slot * vst;
     } else {
-      *kp = k + row * kst + ck * 8;
-      *vp = v + row * vst + cv * 8;
+      kb = k + (uint64_t)(uint32_t)w.at * kst;
+      vb = v + (uint64_t)(uint32_t)w.at * vst;
+      if (__builtin_expect(w.at + 16 > N, 0)) {
+#pragma unroll
+        for (int c = 0; c < FOURS; ++c) {
+          uint32_t ko, vo;
+          offsets(c, N - 1 - w.at, &ko, &vo);
+          dma16(kb, ko, k_to + c * 1024);
+          dma16(vb, vo, v_to + c * 1024);
+        }
+        return;
+      }
     }
+#pragma unroll
+    for (int c = 0; c < FOURS; ++c) dma16(kb, koff[c], k_to + c * 1024);
+#pragma unroll
+    for (int c = 0; c < FOURS; ++c) dma16(vb, voff[c], v_to + c * 1024);
   }
 };
-
-// One wave-wide copy of 64 x 16 bytes from an address per lane to consecutive places in LDS (see dma16 for why it is written out).
-__device__ __forceinline__ void dma16_from(const uint16_t* from, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_base), "v"(from) : "memory", "m0");
-}
-
-// Places in LDS of 16-byte piece `chunk` of row `row`: keys are read 16 rows at one chunk (the four low bits of the row spread
-// them over all banks), values four rows at two neighbouring chunks, transposed (pairs of chunks are spread by three bits of the row).
-__device__ __forceinline__ int key_chunk(int row, int chunk) { return chunk ^ (row & 15); }
-__device__ __forceinline__ int value_chunk(int row, int chunk) { return chunk ^ ((row & 7) << 1); }
 
 // Four rows of one channel: lane i of 16 gets channel i of the 16 channels whose four rows the lanes address, lane 4 m + n the
 // 8 bytes of row m, channels 4 n .. 4 n + 3.
 __device__ __forceinline__ s16x4 read_transposed(uint32_t lds_address) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)lds_address);
+}
+__device__ __forceinline__ bf16x8 read16(uint32_t lds_address) {
+  return *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)lds_address;
 }
 
 // ------------------------------------------------------------------------------------------ infinities and NaN
@@ -179,21 +215,27 @@ __device__ __forceinline__ uint32_t not_finite(const Frag& f) {      // bit 15 o
   for (int i = 0; i < 4; ++i) acc |= (f.u[i] & 0x7f807f80u) + 0x00800080u;
   return acc & 0x80008000u;
 }
-// f without what is not finite; up: 1 where f is +inf or NaN; down: 1 where it is -inf or NaN.
-__device__ __forceinline__ void split_not_finite(Frag& f, Frag& up, Frag& down) {
+// f without what is not finite, and what that was: 1 for +inf, -256 for -inf, both (-255) for NaN.  A product with ones where there is
+// weight, over 64 rows at most, says what a channel has met.
+__device__ __forceinline__ Frag take_not_finite(Frag& f) {
+  Frag met;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t keep = 0, u = 0, d = 0;
+    uint32_t keep = 0, m = 0;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const uint32_t x = (f.u[i] >> (16 * half)) & 0xffffu;
-      const bool bad = (x & 0x7f80u) == 0x7f80u, nan = bad && (x & 0x7fu) != 0;
+      const bool bad = (x & 0x7f80u) == 0x7f80u;
       keep |= (bad ? 0u : x) << (16 * half);
-      u |= (bad && (nan || x < 0x8000u) ? 0x3f80u : 0u) << (16 * half);
-      d |= (bad && (nan || x >= 0x8000u) ? 0x3f80u : 0u) << (16 * half);
+      m |= (bad ? ((x & 0x7fu) ? 0xc37fu : (x < 0x8000u ? 0x3f80u : 0xc380u)) : 0u) << (16 * half);
     }
-    f.u[i] = keep; up.u[i] = u; down.u[i] = d;
+    f.u[i] = keep; met.u[i] = m;
   }
+  return met;
+}
+__device__ __forceinline__ float met_value(float met) {                   // (both make NaN)
+  const float r = met > 0.f ? INFINITY : (truncf(met * 0.00390625f) * 256.f == met ? -INFINITY : NAN);
+  return met == 0.f ? 0.f : r;
 }
 __device__ __forceinline__ Frag given_weight(const Frag& p) {        // 1 where the weight is not 0
   Frag r;

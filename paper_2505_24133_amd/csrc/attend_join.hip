@@ -1,75 +1,112 @@
 // The parts of a query row joined: the largest M, the parts' o weighted by 2^(M_i - M) and divided by their weighted l.
-// A row has 32 threads of four channels each; the few (M, l) of its parts are read by all of them.
+// Half a wave has four channels a lane; its lanes first read one part's (M, l) each, all at once, and then all of its lanes read the
+// parts' o one after the other without waiting in between.  From eight parts on a row has a whole workgroup, an eighth of the parts each half
+// wave, else eight rows share it: bound by latency (three dependent reads), not by bytes.
 #include "attend_internal.h"
 
 namespace rkv {
 
 namespace {
 
-// PER_TOKEN: blocks over all (token, head) rows; otherwise over the rows of the few-rows kernel alone.
-template <bool PER_TOKEN>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int blocks_per) {
+// PER_TOKEN: over all (token, head) rows; otherwise over the rows of the few-rows kernel alone.  SHARE: half waves per row, 1 or 8.
+template <bool PER_TOKEN, int SHARE>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows_per) {
+  __shared__ float4 shared_o[SHARE > 1 ? 8 : 1][32];
+  __shared__ float2 shared_ml[8];
   const int Hq = a.H * a.G;
-  const int outer = blockIdx.x / blocks_per, inner = (blockIdx.x - outer * blocks_per) * 8 + (threadIdx.x >> 5);
-  const int piece = threadIdx.x & 31;
-  int p, token, hq, count, first;
+  const int sub = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = (rows_per + 8 / SHARE - 1) / (8 / SHARE);
+  const int outer = blockIdx.x / per, inner = (blockIdx.x - outer * per) * (8 / SHARE) + (SHARE > 1 ? 0 : sub);
+  int p, token, hq;
+  bool here = inner < rows_per;
+  Tokens tk{0, 0};
   if constexpr (PER_TOKEN) {
     token = outer; hq = inner;
     p = count_not_above(a.starts, a.P + 1, token) - 1;
-    if (p < 0 || p >= a.P) return;
-    const Tokens tk = tokens_between(a, p, p + 1);
-    count = tk.count; first = tk.first;
-    if (hq >= Hq) return;
+    if (p < 0 || p >= a.P) return;                     // (the whole workgroup)
+    tk = tokens_between(a, p, p + 1);
   } else {
     p = outer / a.H;
-    const Tokens tk = tokens_between(a, p, p + 1);
-    count = tk.count; first = tk.first;
-    if (count > kSmallRows || inner >= count * a.G) return;
-    token = first + inner / a.G;
+    tk = tokens_between(a, p, p + 1);
+    here = here && tk.count <= kSmallRows && inner < tk.count * a.G;
+    token = tk.first + inner / a.G;
     hq = (outer - p * a.H) * a.G + inner % a.G;
   }
   const int h = hq / a.G;
   const int64_t row = (int64_t)token * Hq + hq, slots = (int64_t)a.T * Hq;
-  const bool small = a.small_splits > 0 && count <= kSmallRows && count * a.G <= a.small_rows;
-  const int prefixes = group_of(a, p) >= 0 ? a.prefix_splits : 0;
+  const bool small = a.small_splits > 0 && tk.count <= kSmallRows && tk.count * a.G <= a.small_rows;
+  const int prefixes = a.prefix_splits > 0 && group_of(a, p) >= 0 ? a.prefix_splits : 0;
   const int own = small ? a.small_splits : a.tile_splits;
-  if (own == 0 || (own == 1 && a.prefix_splits == 0)) return;     // written whole, or by nobody
-  // the parts behind the prefix's lie `own_step` apart
-  const int64_t own_at = small ? ((int64_t)p * a.small_splits * a.H + h) * a.small_rows + (token - first) * a.G + (hq - h * a.G) : row;
+  here = here && own != 0 && (own != 1 || a.prefix_splits > 0);     // else written whole, or by nobody
+  if (SHARE > 1 && !here) return;
+  const int64_t own_at = small ? ((int64_t)p * a.small_splits * a.H + h) * a.small_rows + (token - tk.first) * a.G + (hq - h * a.G) : row;
   const int64_t own_step = small ? (int64_t)a.H * a.small_rows : slots;
   const float* own_o = small ? a.small_o : a.tile_o;
   const float2* own_ml = small ? a.small_ml : a.tile_ml;
 
-  float top = -INFINITY, l = 0.f;
+  // this half wave's parts: sub, sub + SHARE, ... (at most 32 of them), the prefix's first
+  const int part = SHARE > 1 ? lane * SHARE + sub : lane;
+  const int parts = here ? prefixes + own : 0;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  const float* at = nullptr;
+  if (part < parts) {
+    const bool pre = part < prefixes;
+    const int64_t slot = pre ? row + part * slots : own_at + (part - prefixes) * own_step;
+    ml = (pre ? a.prefix_ml : own_ml)[slot];
+    at = (pre ? a.prefix_o : own_o) + slot * kHeadDim;
+  }
+  float top = half_wave_max(ml.x);
+  const bool some = ml.x != -INFINITY || ml.y != 0.f;              // (a part that saw nothing has written no o)
+  const float weight = some ? exp2_raw(ml.x - safe_max(top)) : 0.f;
+  float l = half_wave_sum(some ? ml.y * weight : 0.f);
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  auto take = [&](const float2* mls, const float* os, int64_t at, int64_t step, int n) {
-    for (int i = 0; i < n; ++i, at += step) {
-      const float2 part = mls[at];
-      if (part.x == -INFINITY && part.y == 0.f) continue;        // nothing visible there (its o is not written)
-      const float next = fmaxf(top, part.x);
-      const float fade = exp2_raw(top - safe_max(next)), weight = exp2_raw(part.x - safe_max(next));
-      x = x * fade + *reinterpret_cast<const f32x4*>(os + at * kHeadDim + piece * 4) * weight;
-      l = l * fade + part.y * weight;
-      top = next;
+  const int base_lane = threadIdx.x & 32;
+  const uint32_t mask = (uint32_t)(__ballot(some) >> base_lane);
+  const int mine = 32 - __clz(mask);
+  for (int i0 = 0; i0 < mine; i0 += 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(i0 + u, 31);
+      const float w = __shfl(weight, base_lane + i);
+      const uint64_t from = (uint64_t)__shfl((unsigned long long)(uintptr_t)at, base_lane + i);
+      if ((mask >> i) & 1u && i == i0 + u) x += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(from) + lane * 4) * w;
     }
-  };
-  take(a.prefix_ml, a.prefix_o, row, slots, prefixes);
-  take(own_ml, own_o, own_at, own_step, own);
+  }
+  if constexpr (SHARE > 1) {
+    shared_o[sub][lane] = make_float4(x[0], x[1], x[2], x[3]);
+    if (lane == 0) shared_ml[sub] = make_float2(top, l);
+    __syncthreads();
+    if (sub != 0) return;
+    float all = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < SHARE; ++i) all = fmaxf(all, shared_ml[i].x);
+    l = 0.f;
+    x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < SHARE; ++i) {
+      const float w = exp2_raw(shared_ml[i].x - safe_max(all));
+      const float4 o = shared_o[i][lane];
+      l += shared_ml[i].y * w;
+      x += f32x4{o.x, o.y, o.z, o.w} * w;
+    }
+    top = all;
+  }
+  if (!here) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  *reinterpret_cast<uint2*>(a.out + token * a.ost + hq * a.osh + piece * 4) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-  if (a.lse != nullptr && piece == 0) a.lse[row] = lse_of(top, l);
+  *reinterpret_cast<uint2*>(a.out + token * a.ost + hq * a.osh + lane * 4) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  if (a.lse != nullptr && lane == 0) a.lse[row] = lse_of(top, l);
 }
 
 }  // namespace
 
 hipError_t launch_attend_join(const AttendArgs& a, bool per_token, hipStream_t stream) {
-  if (per_token) {
-    const int per = (a.H * a.G + 7) / 8;
-    hipLaunchKernelGGL(attend_join_kernel<true>, dim3((unsigned)((int64_t)a.T * per)), dim3(256), 0, stream, a, per);
-  } else {
-    const int per = a.small_rows / 8;
-    hipLaunchKernelGGL(attend_join_kernel<false>, dim3((unsigned)((int64_t)a.P * a.H * per)), dim3(256), 0, stream, a, per);
-  }
+  const bool many = a.prefix_splits + (per_token ? (a.small_splits > a.tile_splits ? a.small_splits : a.tile_splits) : a.small_splits) >= 8;
+  const int rows = per_token ? a.H * a.G : a.small_rows;
+  const int64_t outer = per_token ? a.T : (int64_t)a.P * a.H;
+  const dim3 grid((unsigned)(outer * (many ? rows : (rows + 7) / 8)));
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, rows); };
+  if (per_token) many ? go(attend_join_kernel<true, 8>) : go(attend_join_kernel<true, 1>);
+  else many ? go(attend_join_kernel<false, 8>) : go(attend_join_kernel<false, 1>);
   return hipGetLastError();
 }
 

@@ -15,13 +15,16 @@ namespace {
 constexpr int kTile = 32;                            // rows of a tile
 constexpr int kTileBytes = kTile * kRowBytes;        // of keys, and of values
 constexpr int kWaveBytes = 4 * kTileBytes;           // two buffers of both
-constexpr int kWaves = 4;
+#ifndef KW
+#define KW 2
+#endif
+constexpr int kWaves = KW;
 
 template <int MT, bool PAGED>
-__global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kWaves * 64) void attend_small_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char lds[kWaves * kWaveBytes];
   __shared__ float2 ml[kWaves][MT * 16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int units = a.P * a.H;
   const int split = blockIdx.x / units, unit = blockIdx.x - split * units;
   const int p = unit / a.H, h = unit - p * a.H;
@@ -32,7 +35,8 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
   const int base = prefix_of(a, group_of(a, p));
   const int r0 = len - tk.count;                                 // row of the first new token
   const Sight first = sight(a, r0), last = sight(a, len - 1);
-  const Span<kTile> span(base, a.N, first.lo, last.hi, a.window > 0 ? a.sinks : 0);
+  const int sinks = a.window > 0 ? a.sinks : 0;
+  const Span<kTile> span(base, a.N, first.lo, last.hi, sinks);
 
   // this wave's tiles: a unit's tiles are dealt to as many waves as have one each
   const int used = clampi((span.tiles + kWaves - 1) / kWaves, 1, a.small_splits);
@@ -66,21 +70,14 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
     for (int d = 0; d < 8; ++d) o[m][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  Rows<PAGED> rs(a, p, h);
+  Rows<PAGED, 4> rs(a, p, h, 0);
   const uint32_t mine = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + wave * kWaveBytes;
-  // 16 copies: four rows each, of keys and of values
   auto copy = [&](int tile, int buf) {
-    const int start = span.start(tile), end = span.end(tile);
-    rs.reload(start, min(start + kTile, end) - 1);
+    const int start = span.start(tile);
+    rs.reload(start, start + kTile - 1);
     const uint32_t to = __builtin_amdgcn_readfirstlane(mine + buf * 2 * kTileBytes);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const int r = c * 4 + g4;
-      const uint16_t *kp, *vp;
-      rs.find(min(start + r, end - 1), key_chunk(r, col), value_chunk(r, col), &kp, &vp);
-      dma16_from(kp, to + c * 1024);
-      dma16_from(vp, to + kTileBytes + c * 1024);
-    }
+    for (int c = 0; c < kTile; c += 16) rs.copy(rs.place(start + c), to + c * kRowBytes, to + kTileBytes + c * kRowBytes);   // eight copies
   };
 
   if (t_lo < t_hi) copy(t_lo, 0);
@@ -103,11 +100,11 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int row = b * 16 + col;
-        const bf16x8 kf = *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(kt + row * kRowBytes + (key_chunk(row, 4 * st + g4) << 4));
+        const bf16x8 kf = read16(kt + row * kRowBytes + (key_chunk(row, 4 * st + g4) << 4));
 #pragma unroll
         for (int m = 0; m < MT; ++m) s[m][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[m][st], s[m][b], 0, 0, 0);
       }
-    const bool edge = !(start + kTile <= min(hi_min, span.end(t)) && (start >= lo_max || start + kTile <= a.sinks));
+    const bool edge = !(start + kTile <= min(hi_min, span.end(t)) && (start >= lo_max || start + kTile <= sinks) && start >= base);
     Frag pf[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -118,7 +115,7 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int c = start + (i >> 2) * 16 + 4 * g4 + (i & 3);
-          const bool seen = c < min(see[m].hi, span.end(t)) && (c >= see[m].lo || c < a.sinks);
+          const bool seen = c < min(see[m].hi, span.end(t)) && c >= base && (c >= see[m].lo || c < sinks);
           x[i] = seen ? x[i] : -INFINITY;
         }
       }
@@ -153,19 +150,13 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
         vf.s[half] = read_transposed(vt + row * kRowBytes + (value_chunk(row, chunk) << 4) + ((col & 1) << 3));
       }
       if (edge && __any(not_finite(vf))) {
-        Frag up, down;
-        split_not_finite(vf, up, down);
+        const Frag bad = take_not_finite(vf);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          const Frag w = given_weight(pf[m]);
           const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-          const f32x4 ups = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up.b, w.b, zero, 0, 0, 0);
-          const f32x4 downs = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down.b, w.b, zero, 0, 0, 0);
+          const f32x4 met = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad.b, given_weight(pf[m]).b, zero, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (ups[i] > 0.f) o[m][d][i] += INFINITY;
-            if (downs[i] > 0.f) o[m][d][i] -= INFINITY;
-          }
+          for (int i = 0; i < 4; ++i) o[m][d][i] += met_value(met[i]);
         }
       }
 #pragma unroll
@@ -192,7 +183,7 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
     }
   __syncthreads();
   const bool whole = a.small_splits == 1 && a.prefix_splits == 0;
-  for (int i = threadIdx.x; i < rows * 32; i += 256) {
+  for (int i = threadIdx.x; i < rows * 32; i += kWaves * 64) {
     const int row = i >> 5, piece = i & 31;
     float top = -INFINITY;
 #pragma unroll
@@ -224,7 +215,7 @@ __global__ __launch_bounds__(256) void attend_small_kernel(AttendArgs a) {
 
 hipError_t launch_attend_small(const AttendArgs& a, bool paged, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)a.P * a.H * a.small_splits));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), 0, stream, a); };
   if (a.small_rows <= 16) paged ? go(attend_small_kernel<1, true>) : go(attend_small_kernel<1, false>);
   else if (a.small_rows <= 32) paged ? go(attend_small_kernel<2, true>) : go(attend_small_kernel<2, false>);
   else paged ? go(attend_small_kernel<4, true>) : go(attend_small_kernel<4, false>);

@@ -6,13 +6,15 @@
 // query and half of the tile's rows, so that maxima and sums are register arithmetic and one exchange between the halves of the
 // wave, and the weights are, without any movement, the second operand of O^T += V^T P^T.  V^T comes out of LDS by the transposing read.
 // Two workgroups share a compute unit, so that one's products run beside the other's exponentials.
+#include <type_traits>
+
 #include "attend_internal.h"
 
 namespace rkv {
 
 namespace {
 
-constexpr int kKeys = 64;                            // cache rows of a step
+constexpr int kKeys = 32;                            // cache rows of a step
 constexpr int kKeyBytes = kKeys * kRowBytes;
 constexpr int kThreads = 256;
 constexpr float kSlack = 8.f;        // a maximum that grows by less than 2^8 leaves the weights' reference where it is (they stay below 2^8)
@@ -31,9 +33,11 @@ __device__ __forceinline__ int wave_max(int x) {
 // PREFIX: the query rows are those of a group's problems, the cache rows the group's shared ones.
 template <bool PAGED, bool PREFIX>
 __global__ __launch_bounds__(kThreads, 2) void attend_tiles_kernel(AttendArgs a, int splits) {
-  __shared__ __attribute__((aligned(256))) unsigned char lds[2 * 2 * kKeyBytes];
-  __shared__ int bounds[4][4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ __attribute__((aligned(256))) unsigned char lds[2 * 4 * kKeyBytes];
+  __shared__ int bounds[4][2];
+  __shared__ int2 places[kTileRows];                     // of this lane's query, for the edges and the end: registers are short
+  __shared__ Sight sights[kTileRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % a.H;
   const int rest = blockIdx.x / a.H;
   const int split = rest % splits;
@@ -69,25 +73,29 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles_kernel(AttendArgs a,
   // this lane's query: element j of step s is channel 16 s + 8 (lane >> 5) + j
   const int rows = tk.count * a.G;
   const int col = lane & 31, half = lane >> 5;
-  const int row = tile * kTileRows + wave * 32 + col;
-  const int j = min(row, rows - 1) / a.G;
-  const int g = min(row, rows - 1) - j * a.G;
-  const int token = tk.first + j, hq = h * a.G + g;
   bf16x8 qf[8];
+  int hi_min, hi_max, lo_min, lo_max, p0 = owner, base = 0, lim = a.N;
+  const int sinks = a.window > 0 ? a.sinks : 0;
+  {
+  const int row = min(tile * kTileRows + wave * 32 + col, rows - 1);
+  const int j = row / a.G;
+  const int token = tk.first + j, hq = h * a.G + row - j * a.G;
   const uint16_t* qr = a.q + (int64_t)token * a.qst + (int64_t)hq * a.qsh + half * 8;
 #pragma unroll
   for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + s * 16);
 
-  int p0 = owner, base = 0, lim = a.N;
   Sight see;
   if constexpr (PREFIX) {
     p0 = clampi(a.group_starts[owner], 0, a.P - 1);
     lim = prefix_of(a, owner);
-    // the problem of the lane's token: the last one of the group that starts at or before it
-    int lo = p0, hi = clampi(a.group_starts[owner + 1], p0 + 1, a.P);
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.starts[mid] <= token) lo = mid; else hi = mid;
+    // the problem of the lane's token: as many of the group's later problems start at or before it (their starts are
+    // read 64 at a time and compared from the lanes that hold them)
+    const int p1 = clampi(a.group_starts[owner + 1], p0 + 1, a.P);
+    int lo = p0;
+    for (int at = p0 + 1; at < p1; at += 64) {
+      const int begins = a.starts[min(at + lane, a.P)];
+      const int n = min(64, p1 - at);
+      for (int i = 0; i < n; ++i) lo += __builtin_amdgcn_readlane(begins, i) <= token ? 1 : 0;
     }
     const int end = clampi(a.starts[lo + 1], 0, a.T);
     see = sight(a, clampi(a.kv_len[lo], 0, a.N) - (end - token));
@@ -95,11 +103,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles_kernel(AttendArgs a,
     base = prefix_of(a, group_of(a, owner));
     see = sight(a, clampi(a.kv_len[owner], 0, a.N) - (tk.count - j));
   }
-  const int sinks = a.window > 0 ? a.sinks : 0;
-  const int hi_min = wave_min(see.hi), hi_max = wave_max(see.hi), lo_min = wave_min(see.lo), lo_max = wave_max(see.lo);
+  hi_min = wave_min(see.hi); hi_max = wave_max(see.hi); lo_min = wave_min(see.lo); lo_max = wave_max(see.lo);
+  if (half == 0) {
+    places[wave * 32 + col] = make_int2(token, hq);
+    sights[wave * 32 + col] = see;
+  }
   if (lane == 0) {
     bounds[wave][0] = hi_max;
     bounds[wave][1] = lo_min;
+  }
   }
   __syncthreads();
   const int all_hi = max(max(bounds[0][0], bounds[1][0]), max(bounds[2][0], bounds[3][0]));
@@ -110,127 +122,152 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles_kernel(AttendArgs a,
   const int t_hi = split < used ? (int)((int64_t)span.tiles * (split + 1) / used) : 0;
 
   f32x16 o[4];
-  float mx = -INFINITY, sum = 0.f;
+  float mx = -INFINITY, sum = 0.f;                       // of this lane's rows; the two halves of the wave are added up at the end
+  float minus_ref = 0.f;                                 // what the exponents are taken from: mx, or 0 as long as nothing was visible
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  Rows<PAGED> rs(a, p0, h);
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-  auto copy = [&](int t, int buf) {
-    const int start = span.start(t), end = span.end(t);
-    rs.reload(start, min(start + kKeys, end) - 1);
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * kKeyBytes + wave * 16 * kRowBytes);
+  if (t_lo < t_hi) {
+    Rows<PAGED, 2> rs(a, p0, h, 2 * (wave & 1));
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+    // Batch i: the keys and the values of step i, eight rows a wave, to the rings' places i & 3 (past the last step that one again, for a
+    // constant number of copies).
+    int batch_start = span.start(t_lo);
+    auto batch = [&](int i, int ring) {
+      if (i < t_hi && i != t_lo) batch_start = i == span.tiles_a ? span.start_b : batch_start + kKeys;
+      rs.reload(batch_start, batch_start + kKeys - 1);
+      const auto at = rs.place(batch_start + 16 * (wave >> 1));
+      const uint32_t to = lds0 + wave * 8 * kRowBytes + ring * kKeyBytes;
+      rs.copy(at, to, to + 4 * kKeyBytes);
+    };
+    // Steps [plain_lo, plain_hi) are seen whole by all of the wave's queries.
+    const int plain_lo = span.tiles_a + max(0, (max(base, lo_max) - span.start_b + kKeys - 1) / kKeys);
+    const int plain_hi = span.tiles_a + max(0, min(hi_min, span.end_b) - span.start_b) / kKeys;
+    // places of the fragments in a ring: keys by step of 16 channels, values by block of channels
+    const uint32_t k_at = lds0 + col * kRowBytes + (key_chunk(col, half) << 4);
+    const int vrow = 4 * half + ((lane & 15) >> 2);
+    const uint32_t v_at = lds0 + 4 * kKeyBytes + vrow * kRowBytes + (value_chunk(vrow, 8 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + ((lane & 1) << 3);
+    auto keys = [&](int st, int ring) { return read16((k_at ^ (st << 5)) + ring * kKeyBytes); };
+    // block d has channels 16 d .. 16 d + 15 and 64 + 16 d ..; element j of st is row 16 st + 8 (j >> 2) + 4 half + (j & 3)
+    auto values = [&](int d, int st, int ring) {
+      Frag f;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int r = wave * 16 + c * 4 + (lane >> 4);
-      const uint16_t *kp, *vp;
-      rs.find(min(start + r, end - 1), key_chunk(r, lane & 15), value_chunk(r, lane & 15), &kp, &vp);
-      dma16_from(kp, to + c * 1024);
-      dma16_from(vp, to + kKeyBytes + c * 1024);
-    }
-  };
+      for (int jh = 0; jh < 2; ++jh) f.s[jh] = read_transposed((v_at ^ (d << 5)) + ring * kKeyBytes + (16 * st + 8 * jh) * kRowBytes);
+      return f;
+    };
 
-  if (t_lo < t_hi) copy(t_lo, 0);
-  for (int t = t_lo; t < t_hi; ++t) {
-    const int buf = (t - t_lo) & 1;
-    // this wave's copies have arrived and its reads of the other buffer are done; behind the barrier that holds for all
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < t_hi) copy(t + 1, buf ^ 1);
-    const int start = span.start(t), stop = min(span.end(t), start + kKeys);
-    if (start >= hi_max || (stop <= lo_min && start >= sinks)) continue;      // none of this wave's queries sees any of it
-    const uint32_t kt = lds0 + buf * 2 * kKeyBytes, vt = kt + kKeyBytes;
-    f32x16 s[2];
+    f32x16 s;                                            // element i is row 8 (i >> 2) + 4 half + (i & 3)
+    // One step: its scores s are there; behind them come the next step's scores, beside the weights, and the values' product.
+    auto step = [&](int t, auto ring_of_t) {
+      constexpr int RING = decltype(ring_of_t)::value, NEXT = (RING + 1) & 3;
+      // this wave's copies of step t's values and the next one's keys have arrived (behind them: two copies of values and the batch after)
+      // and its reads of step t - 1 are done; behind the barrier that holds for all
+      asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      batch(t + 3, (RING + 3) & 3);
+      bf16x8 kf[8];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-#pragma unroll
-    for (int st = 0; st < 8; ++st)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int r = b * 32 + col;
-        const bf16x8 kf = *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(kt + r * kRowBytes + (key_chunk(r, 2 * st + half) << 4));
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[b], 0, 0, 0);
-      }
-    // element i of block b is row 32 b + 8 (i >> 2) + 4 half + (i & 3)
-    const bool edge = !(start + kKeys <= min(hi_min, span.end(t)) && (start >= lo_max || start + kKeys <= sinks));
-    if (edge) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int st = 0; st < 4; ++st) kf[st] = keys(st, NEXT);
+      const bool edge = t < plain_lo || t >= plain_hi;
+      if (__builtin_expect(edge, 0)) {
+        asm volatile("" ::: "memory");                   // (a branch, not a selection made for every step)
+        const int start = span.start(t), stop = min(span.end(t), start + kKeys);
+        const Sight see = sights[wave * 32 + col];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int c = start + b * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-          const bool seen = c < min(see.hi, stop) && (c >= see.lo || c < sinks);
-          s[b][i] = seen ? s[b][i] : -INFINITY;
+          const int c = start + 8 * (i >> 2) + 4 * half + (i & 3);
+          const bool seen = c < min(see.hi, stop) && c >= base && (c >= see.lo || c < sinks);
+          s[i] = seen ? s[i] : -INFINITY;
         }
-    }
-    float top = s[0][0];
+      }
+      float top = s[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      top = pair_max32(top) * a.scale2;
+      // the reference moves only where some query's maximum has outgrown it
+      if (__builtin_expect(__any(top > mx + kSlack), 0)) {
+        const float next = fmaxf(mx, top);
+        const float fade = exp2_raw(mx - safe_max(next));
+        mx = next;
+        minus_ref = -safe_max(next);
+        sum *= fade;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
-    top = fmaxf(top, __shfl_xor(top, 32)) * a.scale2;
-    // the reference moves only where some query's maximum has outgrown it
-    if (__any(top > mx + kSlack || mx == -INFINITY)) {
-      const float next = fmaxf(mx, top);
-      const float fade = exp2_raw(mx - safe_max(next));
-      mx = next;
-      sum *= fade;
+        for (int d = 0; d < 4; ++d) o[d] *= fade;
+      }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) o[d] *= fade;
-    }
-    const float ref = safe_max(mx);
-    Frag pf[4];
-    float add = 0.f;
+      for (int st = 4; st < 8; ++st) kf[st] = keys(st, NEXT);
+      f32x16 next;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int i = 0; i < 16; ++i) next[i] = 0.f;
+#pragma unroll
+      for (int st = 0; st < 8; ++st) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf[st], next, 0, 0, 0);
+      Frag w[2], vf[8];
+      float add = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float w = exp2_raw(__fmaf_rn(s[b][i], a.scale2, -ref));
-        add += w;
-        pf[2 * b + (i >> 3)].b[i & 7] = (__bf16)w;
+        const float x = exp2_raw(__fmaf_rn(s[i], a.scale2, minus_ref));
+        add += x;
+        w[i >> 3].b[i & 7] = (__bf16)x;
       }
-    sum += add;                                          // of this lane's rows; the two halves are added up at the end
-    // values: block d has channels 16 d .. 16 d + 15 and 64 + 16 d ..; element j of step st is row 16 st + 8 (j >> 2) + 4 half + (j & 3)
-    const int vrow = 4 * half + ((lane & 15) >> 2);
-    const int vchunk = 8 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      sum += add;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      Frag vf[4];
+      for (int i = 0; i < 8; ++i) vf[i] = values(i & 3, i >> 2, RING);
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+      }
 #pragma unroll
-        for (int jh = 0; jh < 2; ++jh) {
-          const int r = 16 * st + 8 * jh + vrow;
-          vf[st].s[jh] = read_transposed(vt + r * kRowBytes + (value_chunk(r, 2 * d + vchunk) << 4) + ((lane & 1) << 3));
-        }
-      if (edge && __any(not_finite(vf[0]) | not_finite(vf[1]) | not_finite(vf[2]) | not_finite(vf[3]))) {
-        f32x16 ups, downs;
+      for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(w[i].u[0]), "+v"(w[i].u[1]), "+v"(w[i].u[2]), "+v"(w[i].u[3]));
+      asm volatile("" : "+v"(sum));
+      __builtin_amdgcn_sched_barrier(0);
+      if (__builtin_expect(edge, 0)) {
+        // what is not finite is taken out of the values, and added where a weight meets it
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ups[i] = downs[i] = 0.f;
+        for (int i = 0; i < 8; ++i) {
+          if (__any(not_finite(vf[i]))) {
+            f32x16 met;
 #pragma unroll
-        for (int st = 0; st < 4; ++st) {
-          Frag up, down;
-          split_not_finite(vf[st], up, down);
-          const Frag w = given_weight(pf[st]);
-          ups = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up.b, w.b, ups, 0, 0, 0);
-          downs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down.b, w.b, downs, 0, 0, 0);
-        }
+            for (int e = 0; e < 16; ++e) met[e] = 0.f;
+            const Frag bad = take_not_finite(vf[i]);
+            met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad.b, given_weight(w[i >> 2]).b, met, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (ups[i] > 0.f) o[d][i] += INFINITY;
-          if (downs[i] > 0.f) o[d][i] -= INFINITY;
+            for (int e = 0; e < 16; ++e) o[i & 3][e] += met_value(met[e]);
+          }
         }
       }
 #pragma unroll
-      for (int st = 0; st < 4; ++st) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st].b, pf[st].b, o[d], 0, 0, 0);
+      for (int i = 0; i < 8; ++i) o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i].b, w[i >> 2].b, o[i & 3], 0, 0, 0);
+      s = next;
+    };
+
+    batch(t_lo, 0);
+    batch(t_lo + 1, 1);
+    batch(t_lo + 2, 2);
+    asm volatile("s_waitcnt vmcnt(10)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < 8; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys(st, 0), qf[st], s, 0, 0, 0);
+    for (int t = t_lo;;) {
+      step(t, std::integral_constant<int, 0>());
+      if (++t == t_hi) break;
+      step(t, std::integral_constant<int, 1>());
+      if (++t == t_hi) break;
+      step(t, std::integral_constant<int, 2>());
+      if (++t == t_hi) break;
+      step(t, std::integral_constant<int, 3>());
+      if (++t == t_hi) break;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // no copy outlives the workgroup
   }
 
   sum += __shfl_xor(sum, 32);
-  if (row >= rows) return;
+  if (tile * kTileRows + wave * 32 + col >= rows) return;
+  const int token = places[wave * 32 + col].x, hq = places[wave * 32 + col].y;
   const int64_t at = (int64_t)token * (a.H * a.G) + hq;
   if (!PREFIX && splits == 1 && a.prefix_splits == 0) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
