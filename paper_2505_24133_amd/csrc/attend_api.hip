@@ -15,7 +15,6 @@ constexpr int kMaxTokens = 1 << 24;
 constexpr int64_t kMaxBlocks = 1 << 23;
 constexpr int64_t kSlots = 512;             // workgroups of the many-rows kernel that the chip's 256 compute units hold
 constexpr int64_t kSmallSlots = 512;        // and of the few-rows kernel
-constexpr int64_t kSmallShare = 64;         // fewest rows of one of its workgroups
 constexpr int64_t kMaxSplits = 128;         // (the join takes 256 parts)
 
 bool row_stride(int64_t s) { return s >= kHeadDim && s <= 32768 && s % 8 == 0; }
@@ -67,24 +66,27 @@ struct AttendPlan {
   size_t off_small_o, off_small_ml, off_tile_o, off_tile_ml, off_prefix_o, off_prefix_ml, total;
 };
 
-// Into how many workgroups the rows of a few-rows unit are dealt: as many as the chip takes at once, then more where a unit still has a
-// thousand rows for each, so that units of different lengths even out.
-int small_splits(int64_t units, int64_t reach) {
-  const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + kSmallShare - 1) / kSmallShare);
+// Into how many workgroups the rows of a few-rows unit are dealt, at most, and how many rows are worth one: as many as the chip takes at
+// once, with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out.
+void split_small(int64_t units, int64_t reach, AttendArgs* a) {
+  const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + 63) / 64);
   const int64_t even = std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
+  a->small_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
+  a->small_share = fill >= even ? 64 : 512;
 }
 
-// Likewise for the tiles of the many-rows kernel where they do not fill the chip: rounds of workgroups times steps of each, two of
-// them for its start.
-int tile_splits(int64_t tiles, int64_t reach) {
+// Into how many parts the rows of the many-rows kernel's tiles are dealt where there are too few tiles to fill the chip: rounds of
+// workgroups times steps of each (about 1.1 us, with four of them for its start), and what it takes to write the parts and read them
+// again (4 TB/s).
+int split_tiles(int64_t tiles, int64_t rows, int64_t reach) {
   if (tiles >= kSlots) return 1;
   const int64_t steps = (reach + 31) / 32;
   int best = 1;
   double least = 0;
   for (int s = 1; s <= 32 && (s == 1 || s * 4 <= steps); ++s) {
-    const double cost = (double)((tiles * s + kSlots - 1) / kSlots) * (double)((steps + s - 1) / s + 2);
-    if (s == 1 || cost < 0.98 * least) { best = s; least = cost; }
+    const double cost = 1.1 * (double)((tiles * s + kSlots - 1) / kSlots) * (double)((steps + s - 1) / s + 4) +
+                        (s > 1 ? 3.0 + (double)rows * s * (2 * kHeadDim * 4) / 4e6 : 0.0);
+    if (s == 1 || cost < least) { best = s; least = cost; }
   }
   return best;
 }
@@ -115,17 +117,17 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
 
   // Which kernels run.  Up to 64 rows of queries per KV head (new tokens * G) the few-rows kernel has them; where a problem may have
   // more, the many-rows kernel has those problems, and the few-rows kernel the others if there are any.
-  const int64_t most_rows = (int64_t)t.max_new * c.G;
+  const int64_t most_rows = (int64_t)t.max_new * c.G, rows = (int64_t)t.tokens * c.H * c.G;
   const bool large = most_rows > kSmallRows;
   const bool small = !large || (c.P > 1 && c.G <= kSmallRows);
   // rows that a query may see, at most
   const int64_t reach = t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + t.max_new) : c.N;
   if (small) {
     a.small_rows = large || most_rows > 32 ? 64 : (most_rows > 16 ? 32 : 16);
-    a.small_splits = small_splits((int64_t)c.P * c.H, reach);
+    split_small((int64_t)c.P * c.H, reach, &a);
   }
-  if (large) a.tile_splits = tile_splits(attend_tile_bound(t.tokens, c.G, c.P) * c.H, reach);
-  if (t.groups > 0) a.prefix_splits = tile_splits(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, reach);
+  if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach);
+  if (t.groups > 0) a.prefix_splits = split_tiles(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, rows, reach);
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
       (int64_t)t.tokens * ((c.H * c.G + 7) / 8) > kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)
@@ -136,8 +138,7 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
     pl->total = (o + (size_t)bytes + 255) & ~(size_t)255;
     return o;
   };
-  const int64_t rows = (int64_t)t.tokens * c.H * c.G;
-  const int64_t small_parts = a.small_splits > 1 || (small && t.groups > 0) ? (int64_t)c.P * c.H * a.small_rows * a.small_splits : 0;
+  const int64_t small_parts = a.small_splits > 1 || (small && t.groups > 0) ? (large ? (int64_t)c.P * c.H * a.small_rows : rows) * a.small_splits : 0;
   const int64_t tile_parts = a.tile_splits > 1 || (large && t.groups > 0) ? rows * a.tile_splits : 0;
   const int64_t prefix_parts = rows * a.prefix_splits;
   pl->off_small_o = take(small_parts * kHeadDim * 4);
@@ -177,9 +178,7 @@ rkv_status attend(const rkv_params* prm, const rkv_attend_params* att, bool shar
   if (a.prefix_splits > 0 && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
   if (a.tile_splits > 0 && launch_attend_tiles(a, pl.paged, false, st) != hipSuccess) return RKV_ERR_HIP;
   if (a.small_splits > 0 && launch_attend_small(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
-  // parts of single tokens alone are joined unit by unit; where many-rows parts or prefixes are to be joined, token by token
-  const bool per_token = a.prefix_splits > 0 || a.tile_splits > 1;
-  if ((per_token || a.small_splits > 1) && launch_attend_join(a, per_token, st) != hipSuccess) return RKV_ERR_HIP;
+  if ((a.prefix_splits > 0 || a.tile_splits > 1 || a.small_splits > 1) && launch_attend_join(a, st) != hipSuccess) return RKV_ERR_HIP;
   return RKV_OK;
 }
 

@@ -33,9 +33,10 @@ struct AttendArgs {
   KvLayout kl, vl;
   int64_t qst, qsh, ost, osh;
   float scale2;                // scale * log2(e)
-  // parts of the rows, unnormalised: few-rows kernel [p][split][h][small_rows], many-rows kernel [split][t][hq], prefixes likewise
+  // Parts of the rows, unnormalised, [split][t][hq]; those of the few-rows kernel beside the many-rows kernel [p][split][h][small_rows]
   int small_splits, tile_splits, prefix_splits;   // 0: the kernel does not run
-  int small_rows;              // rows per unit in the few-rows parts
+  int small_rows;              // most query rows of a unit of the few-rows kernel: 16, 32 or 64
+  int small_share;             // rows of the cache that are worth a workgroup of it
   float* small_o;
   float2* small_ml;
   float* tile_o;
@@ -259,7 +260,7 @@ __device__ __forceinline__ uint2 pack4(float x, float y, float z, float w) {
 
 hipError_t launch_attend_small(const AttendArgs& a, bool paged, hipStream_t stream);
 hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool prefix, hipStream_t stream);
-hipError_t launch_attend_join(const AttendArgs& a, bool per_token, hipStream_t stream);
+hipError_t launch_attend_join(const AttendArgs& a, hipStream_t stream);
 
 struct RotaryArgs {
   uint16_t* k_cache;

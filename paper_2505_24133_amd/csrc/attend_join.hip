@@ -8,8 +8,11 @@ namespace rkv {
 
 namespace {
 
-// PER_TOKEN: over all (token, head) rows; otherwise over the rows of the few-rows kernel alone.  SHARE: half waves per row, 1 or 8.
-template <bool PER_TOKEN, int SHARE>
+// How the rows are gone through.  One kind of own parts, all [split][t][hq] (kTokens: nothing but the row's own parts is read before them);
+// parts of both kernels, or of the few-rows kernel beside whole rows of the other: by token (kMixed) or by unit (kUnits).
+enum JoinMode { kTokens, kMixed, kUnits };
+
+template <JoinMode MODE, int SHARE>                    // SHARE: half waves per row, 1 or 8
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows_per) {
   __shared__ float4 shared_o[SHARE > 1 ? 8 : 1][32];
   __shared__ float2 shared_ml[8];
@@ -17,30 +20,40 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows
   const int sub = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = (rows_per + 8 / SHARE - 1) / (8 / SHARE);
   const int outer = blockIdx.x / per, inner = (blockIdx.x - outer * per) * (8 / SHARE) + (SHARE > 1 ? 0 : sub);
-  int p, token, hq;
-  bool here = inner < rows_per;
-  Tokens tk{0, 0};
-  if constexpr (PER_TOKEN) {
-    token = outer; hq = inner;
-    p = count_not_above(a.starts, a.P + 1, token) - 1;
-    if (p < 0 || p >= a.P) return;                     // (the whole workgroup)
-    tk = tokens_between(a, p, p + 1);
+  bool here = inner < rows_per, small = false;
+  int token = outer, hq = inner, prefixes = a.prefix_splits;
+  const int64_t slots = (int64_t)a.T * Hq;
+  int64_t row, own_at, own_step = slots;
+  if constexpr (MODE == kTokens) {
+    here = here && token >= a.starts[0] && token < a.starts[a.P];
+    small = a.small_splits > 0;
+    own_at = row = (int64_t)token * Hq + hq;
   } else {
-    p = outer / a.H;
-    tk = tokens_between(a, p, p + 1);
-    here = here && tk.count <= kSmallRows && inner < tk.count * a.G;
-    token = tk.first + inner / a.G;
-    hq = (outer - p * a.H) * a.G + inner % a.G;
+    int p;
+    if constexpr (MODE == kMixed) {
+      p = count_not_above(a.starts, a.P + 1, token) - 1;
+      if (p < 0 || p >= a.P) return;                   // (the whole workgroup)
+    } else {
+      p = outer / a.H;
+    }
+    const Tokens tk = tokens_between(a, p, p + 1);
+    small = a.small_splits > 0 && tk.count <= kSmallRows && tk.count * a.G <= a.small_rows;
+    if constexpr (MODE == kUnits) {
+      here = here && small && inner < tk.count * a.G;
+      token = tk.first + inner / a.G;
+      hq = (outer - p * a.H) * a.G + inner % a.G;
+    }
+    if (prefixes > 0 && group_of(a, p) < 0) prefixes = 0;
+    own_at = row = (int64_t)token * Hq + hq;
+    if (small) {
+      const int h = hq / a.G;
+      own_at = ((int64_t)p * a.small_splits * a.H + h) * a.small_rows + (token - tk.first) * a.G + (hq - h * a.G);
+      own_step = (int64_t)a.H * a.small_rows;
+    }
   }
-  const int h = hq / a.G;
-  const int64_t row = (int64_t)token * Hq + hq, slots = (int64_t)a.T * Hq;
-  const bool small = a.small_splits > 0 && tk.count <= kSmallRows && tk.count * a.G <= a.small_rows;
-  const int prefixes = a.prefix_splits > 0 && group_of(a, p) >= 0 ? a.prefix_splits : 0;
   const int own = small ? a.small_splits : a.tile_splits;
-  here = here && own != 0 && (own != 1 || a.prefix_splits > 0);     // else written whole, or by nobody
+  here = here && (own > 1 || a.prefix_splits > 0);     // else written whole
   if (SHARE > 1 && !here) return;
-  const int64_t own_at = small ? ((int64_t)p * a.small_splits * a.H + h) * a.small_rows + (token - tk.first) * a.G + (hq - h * a.G) : row;
-  const int64_t own_step = small ? (int64_t)a.H * a.small_rows : slots;
   const float* own_o = small ? a.small_o : a.tile_o;
   const float2* own_ml = small ? a.small_ml : a.tile_ml;
 
@@ -99,14 +112,18 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows
 
 }  // namespace
 
-hipError_t launch_attend_join(const AttendArgs& a, bool per_token, hipStream_t stream) {
-  const bool many = a.prefix_splits + (per_token ? (a.small_splits > a.tile_splits ? a.small_splits : a.tile_splits) : a.small_splits) >= 8;
-  const int rows = per_token ? a.H * a.G : a.small_rows;
-  const int64_t outer = per_token ? a.T : (int64_t)a.P * a.H;
-  const dim3 grid((unsigned)(outer * (many ? rows : (rows + 7) / 8)));
+hipError_t launch_attend_join(const AttendArgs& a, hipStream_t stream) {
+  const JoinMode mode = a.small_splits == 0 || a.tile_splits == 0 ? kTokens : (a.prefix_splits > 0 || a.tile_splits > 1 ? kMixed : kUnits);
+  const int parts = a.prefix_splits + (a.small_splits > a.tile_splits || mode == kUnits ? a.small_splits : a.tile_splits);
+  const int rows = mode == kUnits ? a.small_rows : a.H * a.G;
+  const int64_t outer = mode == kUnits ? (int64_t)a.P * a.H : a.T;
+  // (a workgroup per row where its parts are many and rows few, or where half a wave cannot hold them)
+  const bool share = parts > 32 || (parts >= 8 && outer * rows <= 8192);
+  const dim3 grid((unsigned)(outer * (share ? rows : (rows + 7) / 8)));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, rows); };
-  if (per_token) many ? go(attend_join_kernel<true, 8>) : go(attend_join_kernel<true, 1>);
-  else many ? go(attend_join_kernel<false, 8>) : go(attend_join_kernel<false, 1>);
+  if (mode == kTokens) share ? go(attend_join_kernel<kTokens, 8>) : go(attend_join_kernel<kTokens, 1>);
+  else if (mode == kMixed) share ? go(attend_join_kernel<kMixed, 8>) : go(attend_join_kernel<kMixed, 1>);
+  else share ? go(attend_join_kernel<kUnits, 8>) : go(attend_join_kernel<kUnits, 1>);
   return hipGetLastError();
 }
 

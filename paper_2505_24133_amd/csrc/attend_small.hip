@@ -32,14 +32,14 @@ __global__ __launch_bounds__(kWaves * 64) void attend_small_kernel(AttendArgs a)
   const int rows = min(tk.count, kSmallRows) * a.G;              // (a count past it is not this kernel's, and no product overflows)
   if (rows == 0 || tk.count > kSmallRows || rows > MT * 16) return;
   const int len = clampi(a.kv_len[p], 0, a.N);
-  const int base = prefix_of(a, group_of(a, p));
+  const int group = group_of(a, p), base = prefix_of(a, group);
   const int r0 = len - tk.count;                                 // row of the first new token
   const Sight first = sight(a, r0), last = sight(a, len - 1);
   const int sinks = a.window > 0 ? a.sinks : 0;
   const Span<kTile> span(base, a.N, first.lo, last.hi, sinks);
 
-  // this wave's tiles: a unit's tiles are dealt to as many waves as have one each
-  const int used = clampi((span.tiles + kWaves - 1) / kWaves, 1, a.small_splits);
+  // this wave's tiles: a unit's tiles are dealt to as many workgroups as are worth it
+  const int used = clampi((span.tiles * kTile + a.small_share - 1) / a.small_share, 1, a.small_splits);
   const int64_t part = split * kWaves + wave, parts = (int64_t)used * kWaves;
   const int t_lo = split < used ? (int)(span.tiles * part / parts) : 0;
   const int t_hi = split < used ? (int)(span.tiles * (part + 1) / parts) : 0;
@@ -204,9 +204,15 @@ __global__ __launch_bounds__(kWaves * 64) void attend_small_kernel(AttendArgs a)
       *reinterpret_cast<uint2*>(a.out + token * a.ost + hq * a.osh + piece * 4) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
       if (a.lse != nullptr && piece == 0) a.lse[token * (a.H * a.G) + hq] = lse_of(top, l);
     } else {
-      const int64_t at = (((int64_t)p * a.small_splits + split) * a.H + h) * a.small_rows + row;
+      const int j = row / a.G;
+      const int64_t place = (int64_t)(tk.first + j) * (a.H * a.G) + h * a.G + row - j * a.G, places = (int64_t)a.T * (a.H * a.G);
+      const int64_t at = a.tile_splits == 0 ? split * places + place : (((int64_t)p * a.small_splits + split) * a.H + h) * a.small_rows + row;
       if (split < used) *reinterpret_cast<f32x4*>(a.small_o + at * kHeadDim + piece * 4) = x;
-      if (piece == 0) a.small_ml[at] = make_float2(top, l);      // of a workgroup without rows: -inf, 0
+      if (piece == 0) {
+        a.small_ml[at] = make_float2(top, l);                    // of a workgroup without rows: -inf, 0
+        if (split == 0 && group < 0)                             // no prefix: nothing for the join to find
+          for (int i = 0; i < a.prefix_splits; ++i) a.prefix_ml[i * places + place] = make_float2(-INFINITY, 0.f);
+      }
     }
   }
 }

@@ -19,16 +19,9 @@ constexpr int kKeyBytes = kKeys * kRowBytes;
 constexpr int kThreads = 256;
 constexpr float kSlack = 8.f;        // a maximum that grows by less than 2^8 leaves the weights' reference where it is (they stay below 2^8)
 
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int m = 1; m < 32; m <<= 1) x = min(x, __shfl_xor(x, m));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-__device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-  for (int m = 1; m < 32; m <<= 1) x = max(x, __shfl_xor(x, m));
-  return __builtin_amdgcn_readfirstlane(x);
-}
+// Over the 32 queries of a wave (in both of its halves); rows are below 2^24, which a float holds.
+__device__ __forceinline__ int wave_max(int x) { return __builtin_amdgcn_readfirstlane((int)half_wave_max((float)x)); }
+__device__ __forceinline__ int wave_min(int x) { return -wave_max(-x); }
 
 // PREFIX: the query rows are those of a group's problems, the cache rows the group's shared ones.
 template <bool PAGED, bool PREFIX>
@@ -42,14 +35,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles_kernel(AttendArgs a,
   const int rest = blockIdx.x / a.H;
   const int split = rest % splits;
 
-  // the problem (or group) that this tile belongs to, and which of its tiles it is: the tiles of all problems are counted through
+  // The problem (or group) that this tile belongs to, and which of its tiles it is: the tiles of all problems are counted through, 64
+  // at a time.  What else is needed of a problem is read with its tokens: reads that follow each other are what a short call waits for.
   int tile = rest / splits, owner = -1;
   Tokens tk{0, 0};
+  int p0 = 0, p1 = 0, length = 0;                        // the owner's problems (PREFIX), and its rows: of the cache, or of the shared prefix
   const int owners = PREFIX ? a.groups : a.P;
   for (int at = 0; at < owners; at += 64) {
-    const int o = at + lane;
-    Tokens mine{0, 0};
-    if (o < owners) mine = PREFIX ? tokens_between(a, clampi(a.group_starts[o], 0, a.P), clampi(a.group_starts[o + 1], 0, a.P)) : tokens_between(a, o, o + 1);
+    const int o = min(at + lane, owners - 1);
+    int q0 = o, q1 = o + 1;
+    if constexpr (PREFIX) {
+      q0 = clampi(a.group_starts[o], 0, a.P);
+      q1 = clampi(a.group_starts[o + 1], 0, a.P);
+    }
+    const int rows_of = clampi(PREFIX ? a.prefix_len[o] : a.kv_len[o], 0, a.N);
+    Tokens mine = tokens_between(a, q0, q1);
+    if (at + lane >= owners) mine.count = 0;
     const bool small = !PREFIX && a.small_splits > 0 && (int64_t)mine.count * a.G <= a.small_rows;
     const int tiles = small ? 0 : (int)(((int64_t)mine.count * a.G + kTileRows - 1) / kTileRows);
     const int upto = (int)wave_inclusive_scan((uint32_t)tiles);
@@ -57,65 +58,76 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles_kernel(AttendArgs a,
     if (past != 0) {
       const int l = __ffsll((unsigned long long)past) - 1;
       owner = at + l;
-      tk.first = __shfl(mine.first, l);
-      tk.count = __shfl(mine.count, l);
-      tile = __shfl(upto, l) - 1 - tile;               // the last tile, which sees the most rows, first
+      tk.first = __builtin_amdgcn_readlane(mine.first, l);
+      tk.count = __builtin_amdgcn_readlane(mine.count, l);
+      p0 = __builtin_amdgcn_readlane(q0, l);
+      p1 = __builtin_amdgcn_readlane(q1, l);
+      length = __builtin_amdgcn_readlane(rows_of, l);
+      tile = __builtin_amdgcn_readlane(upto, l) - 1 - tile;         // the last tile, which sees the most rows, first
       break;
     }
-    tile -= __shfl(upto, 63);
+    tile -= __builtin_amdgcn_readlane(upto, 63);
   }
   if (owner < 0) return;
-  owner = __builtin_amdgcn_readfirstlane(owner);
-  tk.first = __builtin_amdgcn_readfirstlane(tk.first);
-  tk.count = __builtin_amdgcn_readfirstlane(tk.count);
-  tile = __builtin_amdgcn_readfirstlane(tile);
 
   // this lane's query: element j of step s is channel 16 s + 8 (lane >> 5) + j
   const int rows = tk.count * a.G;
   const int col = lane & 31, half = lane >> 5;
   bf16x8 qf[8];
-  int hi_min, hi_max, lo_min, lo_max, p0 = owner, base = 0, lim = a.N;
+  int hi_min, hi_max, lo_min, lo_max, all_hi, all_lo, base = 0, lim = a.N;
   const int sinks = a.window > 0 ? a.sinks : 0;
   {
-  const int row = min(tile * kTileRows + wave * 32 + col, rows - 1);
-  const int j = row / a.G;
-  const int token = tk.first + j, hq = h * a.G + row - j * a.G;
-  const uint16_t* qr = a.q + (int64_t)token * a.qst + (int64_t)hq * a.qsh + half * 8;
+    const int row = min(tile * kTileRows + wave * 32 + col, rows - 1);
+    const int j = row / a.G;
+    const int token = tk.first + j, hq = h * a.G + row - j * a.G;
+    const uint16_t* qr = a.q + (int64_t)token * a.qst + (int64_t)hq * a.qsh + half * 8;
 #pragma unroll
-  for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + s * 16);
+    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qr + s * 16);
 
-  Sight see;
-  if constexpr (PREFIX) {
-    p0 = clampi(a.group_starts[owner], 0, a.P - 1);
-    lim = prefix_of(a, owner);
-    // the problem of the lane's token: as many of the group's later problems start at or before it (their starts are
-    // read 64 at a time and compared from the lanes that hold them)
-    const int p1 = clampi(a.group_starts[owner + 1], p0 + 1, a.P);
-    int lo = p0;
-    for (int at = p0 + 1; at < p1; at += 64) {
-      const int begins = a.starts[min(at + lane, a.P)];
-      const int n = min(64, p1 - at);
-      for (int i = 0; i < n; ++i) lo += __builtin_amdgcn_readlane(begins, i) <= token ? 1 : 0;
+    Sight see;
+    if constexpr (PREFIX) {
+      lim = length;
+      // the problem of the lane's token is the last one of the group that starts at or before it: the problems' starts and lengths
+      // are read 64 at a time, and every lane bisects the lanes that hold them
+      int end = 0, rows_of = 0;
+      for (int at = p0; at < p1; at += 64) {
+        const int p = min(at + lane, a.P - 1), n = min(64, p1 - at);
+        const int begins = a.starts[p], ends = clampi(a.starts[p + 1], 0, a.T), held = clampi(a.kv_len[p], 0, a.N);
+        int upto = 0;                                    // of these problems
+        for (int step = 32; step > 0; step >>= 1) {
+          const int begin = __shfl(begins, upto + step - 1);
+          if (upto + step <= n && begin <= token) upto += step;
+        }
+        const int begin_63 = __builtin_amdgcn_readlane(begins, 63);
+        if (upto == 63 && n == 64 && begin_63 <= token) upto = 64;
+        const int l = max(upto - 1, 0), end_l = __shfl(ends, l), held_l = __shfl(held, l);
+        if (upto > 0 || at == p0) { end = end_l; rows_of = held_l; }
+      }
+      see = sight(a, rows_of - (end - token));
+      hi_min = wave_min(see.hi); hi_max = wave_max(see.hi); lo_min = wave_min(see.lo); lo_max = wave_max(see.lo);
+      if (lane == 0) {
+        bounds[wave][0] = hi_max;
+        bounds[wave][1] = lo_min;
+      }
+    } else {
+      base = prefix_of(a, group_of(a, owner));
+      const int r0 = length - tk.count;                  // a later token sees no less, and nothing earlier
+      see = sight(a, r0 + j);
+      hi_min = __builtin_amdgcn_readlane(see.hi, 0); hi_max = __builtin_amdgcn_readlane(see.hi, 31);
+      lo_min = __builtin_amdgcn_readlane(see.lo, 0); lo_max = __builtin_amdgcn_readlane(see.lo, 31);
+      all_lo = sight(a, r0 + (int)((uint32_t)(tile * kTileRows) / (uint32_t)a.G)).lo;
+      all_hi = sight(a, r0 + (int)((uint32_t)min(tile * kTileRows + kTileRows - 1, rows - 1) / (uint32_t)a.G)).hi;
     }
-    const int end = clampi(a.starts[lo + 1], 0, a.T);
-    see = sight(a, clampi(a.kv_len[lo], 0, a.N) - (end - token));
-  } else {
-    base = prefix_of(a, group_of(a, owner));
-    see = sight(a, clampi(a.kv_len[owner], 0, a.N) - (tk.count - j));
+    if (half == 0) {
+      places[wave * 32 + col] = make_int2(token, hq);
+      sights[wave * 32 + col] = see;
+    }
   }
-  hi_min = wave_min(see.hi); hi_max = wave_max(see.hi); lo_min = wave_min(see.lo); lo_max = wave_max(see.lo);
-  if (half == 0) {
-    places[wave * 32 + col] = make_int2(token, hq);
-    sights[wave * 32 + col] = see;
+  if constexpr (PREFIX) {
+    __syncthreads();
+    all_hi = max(max(bounds[0][0], bounds[1][0]), max(bounds[2][0], bounds[3][0]));
+    all_lo = min(min(bounds[0][1], bounds[1][1]), min(bounds[2][1], bounds[3][1]));
   }
-  if (lane == 0) {
-    bounds[wave][0] = hi_max;
-    bounds[wave][1] = lo_min;
-  }
-  }
-  __syncthreads();
-  const int all_hi = max(max(bounds[0][0], bounds[1][0]), max(bounds[2][0], bounds[3][0]));
-  const int all_lo = min(min(bounds[0][1], bounds[1][1]), min(bounds[2][1], bounds[3][1]));
   const Span<kKeys> span(base, lim, __builtin_amdgcn_readfirstlane(all_lo), __builtin_amdgcn_readfirstlane(all_hi), sinks);
   const int used = clampi(span.tiles, 1, splits);
   const int t_lo = split < used ? (int)((int64_t)span.tiles * split / used) : 0;
