@@ -86,6 +86,7 @@ class RkvError(RuntimeError):
 
 
 _lib = None
+_append_rotary = _attend_native = None
 _append = None               # _host.append once the library is loaded, or a function that takes no call if that module does not load
 
 
@@ -121,15 +122,17 @@ def load_library() -> ctypes.CDLL:
         getattr(lib, name).restype = ctypes.c_int
     lib.rkv_status_string.argtypes = [ctypes.c_int]
     lib.rkv_status_string.restype = ctypes.c_char_p
-    global _append
+    global _append, _append_rotary, _attend_native
     try:
         from . import _host
     except ImportError:
         # built for another Python or torch, or not at all: no call is taken, every append goes through ctypes
-        _append = lambda *args: None  # noqa: E731
+        _append = _append_rotary = _attend_native = lambda *args: None  # noqa: E731
     else:
         _host.bind(ctypes.cast(lib.rkv_cache_append, ctypes.c_void_p).value, Shape)
         _append = _host.append
+        _host.bind_attend(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.rkv_cache_append_rotary, lib.rkv_attend, lib.rkv_attend_shared)))
+        _append_rotary, _attend_native = _host.append_rotary, _host.attend
     _lib = lib
     return lib
 
@@ -543,6 +546,14 @@ def rkv_cache_append_rotary(shape: Shape, k_cache: torch.Tensor, v_cache: torch.
     """Rotate a ragged batch of new tokens (k_new, v_new [T, kv_heads, d], q_new [T, q_heads, d]; starts cuts them into the problems') by
     their positions seen[p] + j and write keys and values behind the held[p] rows of the caches and the last alpha queries of every
     problem into q_cache (None: nowhere).  Returns the rotated queries (q_out, which may be q_new itself)."""
+    if _append_rotary is None:
+        load_library()
+    # (as with rkv_cache_append: a call in order is checked and enqueued in native code)
+    done = _append_rotary(shape, k_cache, v_cache, q_cache, k_new, v_new, q_new, cos, sin, starts, held, seen, interleaved, q_out)
+    if done is not None:
+        if done[0] != RKV_OK:
+            raise RkvError(done[0], "rkv_cache_append_rotary")
+        return done[1]
     if q_out is None:
         q_out = torch.empty(q_new.shape, dtype=q_new.dtype, device=q_new.device)
     _need_here(k_cache, v_cache, q_cache, k_new, v_new, q_new, cos, sin, starts, held, seen, q_out)
@@ -587,6 +598,13 @@ def make_attend_workspace(shape: Shape, tokens: int, max_new: Optional[int] = No
 
 
 def _attend(shape: Shape, q, k, v, starts, kv_len, group_starts, prefix_len, window, sinks, scale, max_new, ws, out, lse, want_lse, where):
+    if _attend_native is None:
+        load_library()
+    done = _attend_native(shape, q, k, v, starts, kv_len, group_starts, prefix_len, window, sinks, scale, max_new, ws, out, lse, want_lse)
+    if done is not None:
+        if done[0] != RKV_OK:
+            raise RkvError(done[0], where)
+        return done[1:] if done[2] is not None else done[1]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
