@@ -132,6 +132,8 @@ const at::Tensor* here(PyObject* o, at::ScalarType type, int device) {
   if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || t.scalar_type() != type || t.get_device() != device) return nullptr;
   return &t;
 }
+// (asked before the device: a process without a GPU has none to name)
+bool on_gpu(PyObject* o) { return THPVariable_CheckExact(o) && THPVariable_Unpack(o).defined() && THPVariable_Unpack(o).is_cuda(); }
 const int32_t* list_of(PyObject* o, int64_t entries, int device) {
   const at::Tensor* t = here(o, at::kInt, device);
   return t != nullptr && t->dim() == 1 && t->size(0) == entries && t->is_contiguous() ? static_cast<const int32_t*>(t->data_ptr()) : nullptr;
@@ -204,6 +206,7 @@ PyObject* append_rotary(PyObject*, PyObject* const* args, Py_ssize_t count) {
     return nullptr;
   }
   try {
+    if (!on_gpu(args[1])) Py_RETURN_NONE;
     const int device = c10::hip::current_device();
     Caches c;
     bool ok = rotary_fn != nullptr && caches_of(args[0], args[1], args[2], device, &c);
@@ -267,6 +270,7 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t count) {
     return nullptr;
   }
   try {
+    if (!on_gpu(args[2])) Py_RETURN_NONE;
     const int device = c10::hip::current_device();
     Caches c;
     bool ok = attend_fn != nullptr && caches_of(args[0], args[2], args[3], device, &c);
