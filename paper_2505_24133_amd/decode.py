@@ -8,6 +8,9 @@ tokens) and decoding continues.  By default two cache allocations are used alter
 the compaction is a plain gather from one into the other; with ``inplace=True`` there is one
 allocation and the kept rows are moved to its front.  All work runs in the HIP library; this
 class only owns the buffers and the counters.
+
+``append`` takes rows that carry their positions already and leaves attention to the caller; ``step`` takes one token or a
+whole prompt as the projections give them, rotates and appends them, attends over the cache and compresses it when it is full.
 """
 from __future__ import annotations
 
@@ -31,6 +34,10 @@ class DecodeCache:
         self.length = 0            # rows currently held per head
         self.tokens_seen = 0       # decode steps so far
         self.compressions = 0
+        self._counts = None        # row n: n for every problem (what the calls take as lengths), made at the first step
+        self._starts = {}          # by new tokens a problem: where each problem's begin
+        self._attend_ws = {}       # and the workspace of their attention
+        self._groups = None
 
     @property
     def k(self) -> torch.Tensor:
@@ -56,10 +63,62 @@ class DecodeCache:
             return True
         return False
 
+    def share_prompt(self, group_sizes, rows) -> None:
+        """Declare that the next group_sizes[0] problems hold the same values in their first rows[0] rows, the next group_sizes[1] in
+        rows[1], ... (samples of one prompt): step() reads those rows once for all of them, until the first compression, after
+        which every problem has rows of its own."""
+        sizes, rows = [int(n) for n in group_sizes], [int(n) for n in rows]
+        if len(sizes) != len(rows) or min(sizes + rows, default=0) < 0 or sum(sizes) > self.shape.num_problems or max(rows, default=0) > self.length:
+            raise ValueError("share_prompt needs as many row counts as groups, groups of the problems there are and rows that are held")
+        first = [0]
+        for n in sizes:
+            first.append(first[-1] + n)
+        device = self.q_cache.device
+        self._groups = (torch.tensor(first, dtype=torch.int32, device=device), torch.tensor(rows, dtype=torch.int32, device=device)) if sizes else None
+        self._attend_ws = {}
+
+    def step(self, q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor,
+             interleaved: bool = False, window: int = 0, sinks: int = 0, scale=None) -> torch.Tensor:
+        """n new tokens of every problem: q_new [P, n, Hq, d], k_new, v_new [P, n, H, d], not rotated yet.  They are rotated by their
+        positions (cos, sin: rotary_tables with a row for every position so far), appended, and attended over everything that is
+        held (or, with a window, its last rows and the first `sinks`); then the cache is compressed if it is full.
+        Returns the attention's output [P, n, Hq, d]."""
+        s = self.shape
+        P, n = q_new.shape[0], q_new.shape[1]
+        if P != s.num_problems or n < 1 or self.length + n > s.n_tokens:
+            raise ValueError(f"step takes tokens of {s.num_problems} problems, and room for {s.n_tokens - self.length} each is left")
+        if cos.shape[0] < self.tokens_seen + n:
+            raise ValueError(f"the rotation tables end at position {cos.shape[0]}, before the new tokens do")
+        if self._counts is None:
+            device = self.q_cache.device
+            self._counts = torch.arange(s.n_tokens + 1, dtype=torch.int32, device=device)[:, None].expand(-1, P).contiguous()
+        if n not in self._starts:
+            self._starts[n] = torch.arange(0, P * n + 1, n, dtype=torch.int32, device=self.q_cache.device)
+        if n not in self._attend_ws:
+            groups = 0 if self._groups is None else self._groups[1].shape[0]
+            self._attend_ws[n] = rkv.make_attend_workspace(s, P * n, n, groups, self.q_cache.device)
+        starts, k, v = self._starts[n], self.k, self.v
+        # positions count from the last multiple of alpha, whose rows of the tables come first: the slots of the query cache go by them
+        slot = self.tokens_seen % s.alpha
+        at = self.tokens_seen - slot
+        q = rkv.rkv_cache_append_rotary(s, k, v, self.q_cache, k_new.flatten(0, 1), v_new.flatten(0, 1), q_new.flatten(0, 1), cos[at:], sin[at:],
+                                        starts, self._counts[self.length], self._counts[slot], interleaved=interleaved)
+        self.length += n
+        self.tokens_seen += n
+        common = dict(window=window, sinks=sinks, scale=scale, max_new=n, ws=self._attend_ws[n])
+        if self._groups is None:
+            out = rkv.rkv_attend(s, q, k, v, starts, self._counts[self.length], **common)
+        else:
+            out = rkv.rkv_attend_shared(s, q, k, v, starts, self._counts[self.length], *self._groups, **common)
+        if self.length >= s.n_tokens > s.budget:
+            self.compress()
+        return out.view(P, n, s.q_heads, s.head_dim)
+
     def compress(self) -> None:
         s = self.shape
         if self.length != s.n_tokens:
             raise RuntimeError("compress() runs when the cache holds budget + buffer rows")
+        self._groups, self._attend_ws = None, self._attend_ws if self._groups is None else {}
         if self.inplace:
             st, *_ = rkv.rkv_compress_inplace(s, self.q_cache, self.k, self.v, ws=self._ws, kept_idx=self.kept_idx)
             if st != rkv.RKV_OK:

@@ -1,0 +1,80 @@
+"""The decode loop with everything in it: prompts and single tokens rotated, appended, attended and compressed by DecodeCache.step, against
+a cache that is kept row by row on the side and attended in float64."""
+import pytest
+import torch
+
+from attend_reference import Batch, attend64, int32, turned64
+from paper_2505_24133_amd import decode, rkv
+
+pytestmark = pytest.mark.gpu
+
+
+def loop(shape, prompt, steps, inplace=False, window=0, sinks=0, interleaved=False, share=None, rotary=128):
+    P, H, Hq, N, d = shape.num_problems, shape.kv_heads, shape.q_heads, shape.n_tokens, shape.head_dim
+    cache = decode.DecodeCache(shape, inplace=inplace)
+    cos, sin = rkv.rotary_tables(prompt + steps, rotary, 500000.0)
+    side = Batch(H, Hq // H, [1] * P, [1] * P, N=N, seed=prompt)            # rows, queries and lengths of the reference
+    gen, held, seen, compressions = side.gen, 0, 0, 0
+    todo = [prompt] + [1] * steps if prompt else [1] * steps
+    for n in todo:
+        q, k, v = (torch.randn((P, n, x, d), generator=gen, device="cuda").bfloat16() for x in (Hq, H, H))
+        if share and seen == 0:
+            q, k, v = (t.view(-1, share, *t.shape[1:])[:, :1].expand(-1, share, -1, -1, -1).reshape(t.shape) for t in (q, k, v))
+        # what the rotation gives, by a call of its own into rows of its own, and within its bounds
+        flat = [t.flatten(0, 1).contiguous() for t in (q, k, v)]
+        rows = torch.zeros((2, P, H, N, d), dtype=torch.bfloat16, device="cuda")
+        q_turned = rkv.rkv_cache_append_rotary(shape, rows[0], rows[1], None, flat[1], flat[2], flat[0], cos, sin,
+                                               int32([i * n for i in range(P + 1)]), int32([held] * P), int32([seen] * P), interleaved=interleaved)
+        c, s = (t[seen:seen + n].repeat(P, 1) for t in (cos, sin))
+        new_rows = slice(held, held + n)
+        for got, x in ((q_turned, flat[0]), (rows[0][:, :, new_rows].transpose(1, 2).flatten(0, 1), flat[1])):
+            want, err = turned64(x, c, s, interleaved)
+            assert bool(((got.double() - want).abs() <= err).all())
+        side.rows_k[:, :, new_rows], side.rows_v[:, :, new_rows] = rows[0][:, :, new_rows], v.transpose(1, 2)
+        held, seen = held + n, seen + n
+        side.q, side.new, side.lens, side.T = q_turned, [n] * P, [held] * P, P * n
+        full = held >= N
+        out = cache.step(q, k, v, cos, sin, interleaved=interleaved, window=window, sinks=sinks)
+        assert out.shape == (P, n, Hq, d) and cache.tokens_seen == seen
+        ref, _, e_out, _ = attend64(side, window, sinks)
+        assert bool(((out.flatten(0, 1).double() - ref).abs() <= e_out).all())
+        for j in range(max(0, n - shape.alpha), n):
+            assert torch.equal(cache.q_cache[:, :, (seen - n + j) % shape.alpha], q_turned.view(P, n, Hq, d)[:, j])
+        if full:
+            compressions += 1
+            kept = cache.kept_idx.long()[..., None].expand(-1, -1, -1, d)
+            held = shape.budget
+            side.rows_k[:, :, :held], side.rows_v[:, :, :held] = side.rows_k.gather(2, kept), side.rows_v.gather(2, kept)
+        assert cache.length == held and cache.compressions == compressions
+        assert torch.equal(cache.k[:, :, :held], side.rows_k[:, :, :held]) and torch.equal(cache.v[:, :, :held], side.rows_v[:, :, :held])
+        if share and seen == prompt:
+            cache.share_prompt([share] * (P // share), [prompt] * (P // share))
+
+
+def shape(P, H, G, N, budget):
+    return rkv.Shape(num_problems=P, kv_heads=H, q_heads=H * G, n_tokens=N, budget=budget)
+
+
+@pytest.mark.parametrize("how", [
+    pytest.param(dict(shape=shape(2, 2, 4, 48, 32), prompt=20, steps=70), id="a prompt, then three compressions"),
+    pytest.param(dict(shape=shape(1, 3, 5, 96, 64), prompt=96, steps=40, inplace=True, interleaved=True), id="a prompt that fills the cache, in place"),
+    pytest.param(dict(shape=shape(3, 1, 2, 40, 30), prompt=0, steps=60, window=17, sinks=2, rotary=64), id="tokens only, a window"),
+    pytest.param(dict(shape=shape(6, 2, 4, 300, 256), prompt=200, steps=120, share=3), id="samples of two prompts"),
+])
+def test_loop(how):
+    loop(**how)
+
+
+def test_refusals():
+    s = shape(1, 1, 2, 40, 30)
+    cache = decode.DecodeCache(s)
+    cos, sin = rkv.rotary_tables(20)
+    q, k = torch.zeros((1, 41, 2, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 41, 1, 128), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="room for 40"):
+        cache.step(q, k, k, cos, sin)
+    with pytest.raises(ValueError, match="end at position 20"):
+        cache.step(q[:, :21], k[:, :21], k[:, :21], cos, sin)
+    cache.step(q[:, :20], k[:, :20], k[:, :20], cos, sin)
+    for sizes, rows in (([2], [5]), ([1], [21]), ([1], [5, 6]), ([-1], [3])):
+        with pytest.raises(ValueError, match="share_prompt"):
+            cache.share_prompt(sizes, rows)
