@@ -67,10 +67,11 @@ struct AttendPlan {
 };
 
 // Into how many workgroups the rows of a few-rows unit are dealt, at most, and how many rows are worth one: as many as the chip takes at
-// once, with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out.
+// once, with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out (not behind
+// shared prefixes: what is left of the rows there is not known here, and workgroups that find nothing to do are not free).
 void split_small(int64_t units, int64_t reach, AttendArgs* a) {
   const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + 63) / 64);
-  const int64_t even = std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
+  const int64_t even = a->groups > 0 ? 0 : std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
   a->small_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
   a->small_share = fill >= even ? 64 : 512;
 }
@@ -175,9 +176,13 @@ rkv_status attend(const rkv_params* prm, const rkv_attend_params* att, bool shar
   a.prefix_o = reinterpret_cast<float*>(w + pl.off_prefix_o);
   a.prefix_ml = reinterpret_cast<float2*>(w + pl.off_prefix_ml);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (a.prefix_splits > 0 && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
-  if (a.tile_splits > 0 && launch_attend_tiles(a, pl.paged, false, st) != hipSuccess) return RKV_ERR_HIP;
-  if (a.small_splits > 0 && launch_attend_small(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
+  if (a.prefix_splits > 0 && a.tile_splits == 0 && a.small_rows <= 32) {
+    if (launch_attend_prefix(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
+  } else {
+    if (a.prefix_splits > 0 && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
+    if (a.tile_splits > 0 && launch_attend_tiles(a, pl.paged, false, st) != hipSuccess) return RKV_ERR_HIP;
+    if (a.small_splits > 0 && launch_attend_small(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
+  }
   if ((a.prefix_splits > 0 || a.tile_splits > 1 || a.small_splits > 1) && launch_attend_join(a, st) != hipSuccess) return RKV_ERR_HIP;
   return RKV_OK;
 }

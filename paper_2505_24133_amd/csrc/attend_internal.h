@@ -260,6 +260,8 @@ __device__ __forceinline__ uint2 pack4(float x, float y, float z, float w) {
 
 hipError_t launch_attend_small(const AttendArgs& a, bool paged, hipStream_t stream);
 hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool prefix, hipStream_t stream);
+// Prefixes and few-rows parts in one launch (small_rows <= 32).
+hipError_t launch_attend_prefix(const AttendArgs& a, bool paged, hipStream_t stream);
 hipError_t launch_attend_join(const AttendArgs& a, hipStream_t stream);
 
 struct RotaryArgs {
