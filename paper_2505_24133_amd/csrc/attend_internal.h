@@ -164,8 +164,8 @@ struct Rows {
     if constexpr (PAGED) return Place{at, __builtin_amdgcn_readlane(ids, ((at >> shift) - first) & 63)};
     return Place{at, 0};
   }
-  // Its keys and values to LDS.  Past the end of a contiguous cache a lane pulls its row back to the last one, in a page there is room:
-  // the caller hides what is past the end.
+  // Its keys and values to LDS, all keys before the values (who waits for the keys alone counts on it).  Past the end of a contiguous cache a
+  // lane pulls its row back to the last one, in a page there is room: the caller hides what is past the end.
   __device__ __forceinline__ void copy(Place w, uint32_t k_to, uint32_t v_to) const {
     const unsigned char *kb, *vb;
     if constexpr (PAGED) {
@@ -176,13 +176,13 @@ struct Rows {
       kb = k + (uint64_t)(uint32_t)w.at * kst;
       vb = v + (uint64_t)(uint32_t)w.at * vst;
       if (__builtin_expect(w.at + 16 > N, 0)) {
+        uint32_t ko[FOURS], vo[FOURS];
 #pragma unroll
-        for (int c = 0; c < FOURS; ++c) {
-          uint32_t ko, vo;
-          offsets(c, N - 1 - w.at, &ko, &vo);
-          dma16(kb, ko, k_to + c * 1024);
-          dma16(vb, vo, v_to + c * 1024);
-        }
+        for (int c = 0; c < FOURS; ++c) offsets(c, N - 1 - w.at, &ko[c], &vo[c]);
+#pragma unroll
+        for (int c = 0; c < FOURS; ++c) dma16(kb, ko[c], k_to + c * 1024);
+#pragma unroll
+        for (int c = 0; c < FOURS; ++c) dma16(vb, vo[c], v_to + c * 1024);
         return;
       }
     }

@@ -286,29 +286,43 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int splits, int bloc
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // no copy outlives the workgroup
   }
 
+  // The wave's rows go out through LDS (its 16 KB of the rings, behind a barrier), so that whole rows are written: row col's 16-byte
+  // pieces lie xor-ed by the row.
   sum += __shfl_xor(sum, 32);
-  if (tile * kTileRows + wave * 32 + col >= rows) return;
-  const int token = places[wave * 32 + col].x, hq = places[wave * 32 + col].y;
-  const int64_t at = (int64_t)token * (a.H * a.G) + hq;
-  if (!PREFIX && splits == 1 && a.prefix_splits == 0) {
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    uint16_t* to = a.out + (int64_t)token * a.ost + (int64_t)hq * a.osh + 4 * half;
+  const bool whole = !PREFIX && splits == 1 && a.prefix_splits == 0;
+  const int64_t slots = (int64_t)split * a.T * (a.H * a.G);
+  const int left = rows - tile * kTileRows - wave * 32;  // of this wave's 32 rows there are so many
+  if (col < left && half == 0) {
+    const int2 place = places[wave * 32 + col];
+    const int64_t at = (int64_t)place.x * (a.H * a.G) + place.y;
+    if (!whole) (PREFIX ? a.prefix_ml : a.tile_ml)[slots + at] = make_float2(mx, sum);
+    else if (a.lse != nullptr) a.lse[at] = lse_of(mx, sum);
+  }
+  if (!whole && t_lo == t_hi) return;                    // (of a part without rows -inf, 0 is all that is read)
+  asm volatile("s_barrier" ::: "memory");
+  float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kHeadDim;
+  const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<uint2*>(to + 64 * (i >> 3) + 16 * d + 8 * ((i >> 2) & 1)) = pack4(o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv);
-    if (a.lse != nullptr && half == 0) a.lse[at] = lse_of(mx, sum);
+    for (int i = 0; i < 16; i += 4) {
+      const int piece = 16 * (i >> 3) + 4 * d + 2 * ((i >> 2) & 1) + half;
+      *reinterpret_cast<f32x4*>(mine + col * kHeadDim + ((piece ^ col) & 31) * 4) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * inv;
+    }
+  if (whole) {
+    for (int r = lane >> 4; r < min(left, 32); r += 4) {
+      const int2 place = places[wave * 32 + r];
+      const int piece = 2 * (lane & 15);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(mine + r * kHeadDim + (piece ^ r) * 4), y = *reinterpret_cast<const f32x4*>(mine + r * kHeadDim + ((piece + 1) ^ r) * 4);
+      const uint2 lo = pack4(x[0], x[1], x[2], x[3]), hi = pack4(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint4*>(a.out + (int64_t)place.x * a.ost + (int64_t)place.y * a.osh + piece * 4) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
   } else {
-    const int64_t slot = (int64_t)split * a.T * (a.H * a.G) + at;
-    float* to = (PREFIX ? a.prefix_o : a.tile_o) + slot * kHeadDim + 4 * half;
-    if (t_lo < t_hi)
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<f32x4*>(to + 64 * (i >> 3) + 16 * d + 8 * ((i >> 2) & 1)) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
-    if (half == 0) (PREFIX ? a.prefix_ml : a.tile_ml)[slot] = make_float2(mx, sum);
+    for (int r = lane >> 5; r < min(left, 32); r += 2) {
+      const int2 place = places[wave * 32 + r];
+      const int64_t slot = slots + (int64_t)place.x * (a.H * a.G) + place.y;
+      *reinterpret_cast<f32x4*>((PREFIX ? a.prefix_o : a.tile_o) + slot * kHeadDim + (lane & 31) * 4) = *reinterpret_cast<const f32x4*>(mine + r * kHeadDim + ((lane & 31) ^ r) * 4);
+    }
   }
 }
 

@@ -164,6 +164,15 @@ def test_a_query_has_the_same_bits_in_any_company():
         assert all(torch.equal(x, y) for x, y in zip(first, again))
 
 
+@pytest.mark.parametrize("N,new,G", [(1500, 130, 5), (77, 60, 2), (333, 1, 4), (45, 3, 5)])
+def test_the_last_rows_of_a_cache_are_there_every_time(N, new, G):
+    """Contiguous caches whose length is no multiple of 16: their last rows are copied in a way of their own, and are there when they are read."""
+    b = Batch(1, G, [new], [N], seed=N)
+    want = attend64(b, window=1)
+    for _ in range(40):
+        check(run(b, window=1), want)
+
+
 def test_lists_outside_their_ranges_read_nothing_outside():
     """Lengths past the cache, below zero, pages that are not in the pool: nothing is read out of bounds; the rest is as it should be."""
     b = Batch(2, 4, [1, 1, 1], [40, 64, 64], N=64, page=16, seed=15)
