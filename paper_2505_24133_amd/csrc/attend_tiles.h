@@ -217,6 +217,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int splits, int bloc
         for (int d = 0; d < 4; ++d) o[d] *= fade;
       }
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);                     // a wave that has its products goes before the one that looks for its maxima: 3 to 9 %
 #pragma unroll
       for (int st = 4; st < 8; ++st) kf[st] = keys(st, NEXT);
       f32x16 next;
@@ -262,6 +263,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int splits, int bloc
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i].b, w[i >> 2].b, o[i & 3], 0, 0, 0);
+      __builtin_amdgcn_s_setprio(0);
       s = next;
     };
 
