@@ -63,14 +63,15 @@ rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_param
  * -infinity.  What a token does not see has no influence on it, infinities and NaN included.  Sums and the softmax are held in fp32; the
  * weights are rounded to bf16 before they are multiplied with v.
  *
- * max_new bounds the new tokens of one problem; tokens of a problem past it may be left unwritten.  The closer it is the better: up
+ * max_new bounds the new tokens of one problem; the outputs of a problem that has more are unspecified.  The closer it is the better: up
  * to 64 rows of queries per KV head (max_new * G) a kernel for few rows runs alone.  T is always a valid bound.
  *
  * rkv_attend_shared: the problems group_starts[g] .. group_starts[g + 1] - 1 (device, int32 [groups + 1], ascending) hold the same values in
  * rows 0 .. prefix_len[g] - 1 (a prompt that they share: copies, or the same pages).  Those rows are read once for the whole group, from its
  * first problem's cache; the result is rkv_attend's.  Problems in no group are attended by themselves.
  *
- * Both need a workspace of rkv_attend_workspace_size() bytes (0 for calls that need none), 256-byte aligned.  groups is 0 for rkv_attend.
+ * Both need a workspace of rkv_attend_workspace_size() bytes (0 for calls that need none), 256-byte aligned; the size for a window of 0 does for
+ * any window.  out must not overlap the other arrays.  groups is 0 for rkv_attend.
  */
 typedef struct {
   int32_t tokens;            /* T >= 0 */

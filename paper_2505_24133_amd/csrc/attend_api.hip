@@ -68,7 +68,8 @@ struct AttendPlan {
 
 // Into how many workgroups the rows of a few-rows unit are dealt, at most, and how many rows are worth one: as many as the chip takes at
 // once, with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out (not behind
-// shared prefixes: what is left of the rows there is not known here, and workgroups that find nothing to do are not free).
+// shared prefixes: what is left of the rows there is not known here, and workgroups that find nothing to do are not free: 64 samples of
+// one prompt 4 us).  48 ragged caches of up to 8320 rows under a window of 4096: 174 us with one workgroup a unit, 150 with four.
 void split_small(int64_t units, int64_t reach, AttendArgs* a) {
   const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + 63) / 64);
   const int64_t even = a->groups > 0 ? 0 : std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
@@ -78,7 +79,8 @@ void split_small(int64_t units, int64_t reach, AttendArgs* a) {
 
 // Into how many parts the rows of the many-rows kernel's tiles are dealt where there are too few tiles to fill the chip: rounds of
 // workgroups times steps of each (about 1.1 us, with four of them for its start), and what it takes to write the parts and read them
-// again (4 TB/s).
+// again (4 TB/s).  511 tokens of seven heads behind 7681 rows, 112 tiles: 4 parts 75 us, 9 parts (two full rounds) 102 us, 5 parts (one round
+// and a little) 112 us.
 int split_tiles(int64_t tiles, int64_t rows, int64_t reach) {
   if (tiles >= kSlots) return 1;
   const int64_t steps = (reach + 31) / 32;
@@ -90,6 +92,11 @@ int split_tiles(int64_t tiles, int64_t rows, int64_t reach) {
     if (s == 1 || cost < least) { best = s; least = cost; }
   }
   return best;
+}
+// (no more under a window than without one, so that a workspace sized without it does)
+int split_tiles(int64_t tiles, int64_t rows, int64_t reach, int64_t all) {
+  const int s = split_tiles(tiles, rows, reach);
+  return reach == all ? s : std::min(s, split_tiles(tiles, rows, all));
 }
 
 rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool shared, AttendPlan* pl) {
@@ -126,9 +133,11 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   if (small) {
     a.small_rows = large || most_rows > 32 ? 64 : (most_rows > 16 ? 32 : 16);
     split_small((int64_t)c.P * c.H, reach, &a);
+    // (a token array that is mostly padding would make for large parts by token)
+    a.small_by_token = !large && rows <= (int64_t)c.P * c.H * a.small_rows;
   }
-  if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach);
-  if (t.groups > 0) a.prefix_splits = split_tiles(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, rows, reach);
+  if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach, c.N);
+  if (t.groups > 0) a.prefix_splits = split_tiles(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, rows, reach, c.N);
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
       (int64_t)t.tokens * ((c.H * c.G + 7) / 8) > kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)
@@ -139,7 +148,7 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
     pl->total = (o + (size_t)bytes + 255) & ~(size_t)255;
     return o;
   };
-  const int64_t small_parts = a.small_splits > 1 || (small && t.groups > 0) ? (large ? (int64_t)c.P * c.H * a.small_rows : rows) * a.small_splits : 0;
+  const int64_t small_parts = a.small_splits > 1 || (small && t.groups > 0) ? (a.small_by_token ? rows : (int64_t)c.P * c.H * a.small_rows) * a.small_splits : 0;
   const int64_t tile_parts = a.tile_splits > 1 || (large && t.groups > 0) ? rows * a.tile_splits : 0;
   const int64_t prefix_parts = rows * a.prefix_splits;
   pl->off_small_o = take(small_parts * kHeadDim * 4);

@@ -33,9 +33,10 @@ struct AttendArgs {
   KvLayout kl, vl;
   int64_t qst, qsh, ost, osh;
   float scale2;                // scale * log2(e)
-  // Parts of the rows, unnormalised, [split][t][hq]; those of the few-rows kernel beside the many-rows kernel [p][split][h][small_rows]
+  // Parts of the rows, unnormalised, [split][t][hq]; those of the few-rows kernel without small_by_token [p][split][h][small_rows]
   int small_splits, tile_splits, prefix_splits;   // 0: the kernel does not run
   int small_rows;              // most query rows of a unit of the few-rows kernel: 16, 32 or 64
+  bool small_by_token;
   int small_share;             // rows of the cache that are worth a workgroup of it
   float* small_o;
   float2* small_ml;

@@ -8,8 +8,8 @@ namespace rkv {
 
 namespace {
 
-// How the rows are gone through.  One kind of own parts, all [split][t][hq] (kTokens: nothing but the row's own parts is read before them);
-// parts of both kernels, or of the few-rows kernel beside whole rows of the other: by token (kMixed) or by unit (kUnits).
+// How the rows are gone through.  All parts [split][t][hq], own ones of one kind (kTokens: nothing but the row's own parts is read before
+// them); of both kinds, or by unit, with others beside them (kMixed) or alone (kUnits: over the few-rows kernel's units).
 enum JoinMode { kTokens, kMixed, kUnits };
 
 template <JoinMode MODE, int SHARE>                    // SHARE: half waves per row, 1 or 8
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows
 }  // namespace
 
 hipError_t launch_attend_join(const AttendArgs& a, hipStream_t stream) {
-  const JoinMode mode = a.small_splits == 0 || a.tile_splits == 0 ? kTokens : (a.prefix_splits > 0 || a.tile_splits > 1 ? kMixed : kUnits);
+  const JoinMode mode = a.small_splits == 0 || a.small_by_token ? kTokens : (a.prefix_splits > 0 || a.tile_splits > 1 ? kMixed : kUnits);
   const int parts = a.prefix_splits + (a.small_splits > a.tile_splits || mode == kUnits ? a.small_splits : a.tile_splits);
   const int rows = mode == kUnits ? a.small_rows : a.H * a.G;
   const int64_t outer = mode == kUnits ? (int64_t)a.P * a.H : a.T;

@@ -212,7 +212,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int block, Lds<MT>& 
     } else {
       const int j = row / a.G;
       const int64_t place = (int64_t)(tk.first + j) * (a.H * a.G) + h * a.G + row - j * a.G, places = (int64_t)a.T * (a.H * a.G);
-      const int64_t at = a.tile_splits == 0 ? split * places + place : (((int64_t)p * a.small_splits + split) * a.H + h) * a.small_rows + row;
+      const int64_t at = a.small_by_token ? split * places + place : (((int64_t)p * a.small_splits + split) * a.H + h) * a.small_rows + row;
       if (split < used) *reinterpret_cast<f32x4*>(a.small_o + at * kHeadDim + piece * 4) = x;
       if (piece == 0) {
         a.small_ml[at] = make_float2(top, l);                    // of a workgroup without rows: -inf, 0

@@ -126,6 +126,14 @@ def test_workspace_grows_with_the_parts_only(lib):
     assert long > 0
     for window in (1, 100, 4096, 2 ** 31 - 1):
         assert size(lib, block(shape(num_problems=1, n_tokens=32768)), att(tokens=1, window=window, sinks=2 ** 31 - 1))[1] <= long
+    # nor does a chunk of a prompt
+    for T in (100, 511, 1000, 2000, 5000):
+        for N in (5000, 8192, 20000, 100000):
+            p = block(shape(num_problems=1, n_tokens=N, kv_heads=4, q_heads=28))
+            most = size(lib, p, att(tokens=T, max_new=T))[1]
+            assert all(size(lib, p, att(tokens=T, max_new=T, window=w, sinks=4))[1] <= most for w in (1, 500, 1024, 3000, 4096, 7000, 50000))
+    # a token array that is mostly padding
+    assert size(lib, block(shape(num_problems=2, n_tokens=32768)), att(tokens=100000, max_new=1))[1] < 100e6
     # never more than some hundred MB, whatever is asked for without a shared prefix
     for P in (1, 2, 64):
         for T in (1, 64, 1000, 16000):

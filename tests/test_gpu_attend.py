@@ -146,6 +146,15 @@ def test_strided_queries_and_outputs_and_rows_behind_the_batch():
         assert (room[n:] == 9).all() and (room[:, :2] == 9).all() and (room[:, 8:] == 9).all() and (lse[n:] == 4).all()
 
 
+def test_a_token_array_that_is_mostly_padding():
+    """Parts that do not lie by token, joined unit by unit; what is behind the batch stays as it was."""
+    b = Batch(2, 4, [1, 2, 1], [3000, 700, 5000], seed=21, page=16, extra_tokens=3000)
+    out, lse = torch.full_like(b.q, 3.0), torch.full(b.q.shape[:2], 4.0, device="cuda")
+    run(b, out=out, lse=lse)
+    check((out[:4], lse[:4]), tuple(t[:4] for t in attend64(b)))
+    assert (out[4:] == 3).all() and (lse[4:] == 4).all()
+
+
 def test_any_bound_on_the_new_tokens_gives_the_same_up_to_rounding():
     b = Batch(2, 4, [1, 2, 1], [50, 300, 1000], seed=13, page=16)
     want = attend64(b)

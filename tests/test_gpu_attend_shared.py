@@ -87,6 +87,29 @@ def test_hidden_values_that_are_not_finite():
     assert (out[0, :, 3] == float("inf")).all()
 
 
+def test_groups_in_the_middle_and_padding():
+    """Problems before and behind the groups, tokens before the first problem's and behind the last one's."""
+    b = grouped(2, 4, [3, 2], [150, 60], [1, 2], [30, 5], outside=2, seed=9, extra_tokens=2000)
+    P = b.P
+    # the first problem keeps to itself: the groups start behind it
+    b2 = grouped(2, 4, [1, 3, 2], [0, 150, 60], [1, 2], [30, 5], outside=1, seed=10, extra_tokens=700)
+    b2.group_starts, b2.prefix_len = int32([1, 4, 6]), int32([150, 60])
+    for x in (b, b2):
+        n = sum(x.new)
+        out, lse = torch.full_like(x.q, 3.0), torch.full(x.q.shape[:2], 4.0, device="cuda")
+        run(x, out=out, lse=lse)
+        check((out[:n], lse[:n]), tuple(t[:n] for t in attend64(x)))
+        assert (out[n:] == 3).all() and (lse[n:] == 4).all()
+    # tokens that belong to no problem, in front
+    shifted = int32([0] * (P + 1)) + b.starts + 5
+    q = torch.cat((torch.zeros_like(b.q[:5]), b.q))[:b.T]
+    out = torch.full_like(q, 3.0)
+    rkv.rkv_attend_shared(b.shape, q, b.k, b.v, shifted, b.kv_len, b.group_starts, b.prefix_len, max_new=2, out=out)
+    n = sum(b.new)
+    want = attend64(b)
+    assert bool(((out[5:5 + n].double() - want[0][:n]).abs() <= want[2][:n]).all()) and (out[:5] == 3).all() and (out[5 + n:] == 3).all()
+
+
 def test_no_groups():
     b = Batch(2, 4, [1, 2], [100, 300], seed=7)
     b.group_starts, b.prefix_len = int32([0]), int32([])
