@@ -211,11 +211,25 @@ union Frag {
   uint32_t u[4];
   s16x4 s[2];
 };
-__device__ __forceinline__ uint32_t not_finite(const Frag& f) {      // bit 15 or 31 of the result is set if an element is not finite
-  uint32_t acc = 0;
+// The largest magnitudes, as bits, of the elements of f and of what came before, in both halves of a word (bf16 is ordered as its bits are).
+__device__ __forceinline__ uint32_t largest_magnitudes(uint32_t so_far, const Frag& f) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  union { uint32_t u; u16x2 v; } a, b;
+  a.u = so_far;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) acc |= (f.u[i] & 0x7f807f80u) + 0x00800080u;
-  return acc & 0x80008000u;
+  for (int i = 0; i < 4; ++i) {
+    b.u = f.u[i] & 0x7fff7fffu;
+    a.v = __builtin_elementwise_max(a.v, b.v);
+  }
+  return a.u;
+}
+__device__ __forceinline__ bool not_finite(uint32_t largest) { return (largest & 0xffffu) >= 0x7f80u || (largest >> 16) >= 0x7f80u; }
+
+// Bits n and above (n may be negative, or past 31), and a score where its row's bit is set, else -infinity.
+__device__ __forceinline__ uint32_t bits_from(int n) { return n >= 32 ? 0u : 0xffffffffu << max(n, 0); }
+__device__ __forceinline__ float seen_or(float score, uint32_t seen, int bit) {
+  const uint32_t all = (uint32_t)((int32_t)(seen << (31 - bit)) >> 31);
+  return __uint_as_float((__float_as_uint(score) & all) | (0xff800000u & ~all));
 }
 // f without what is not finite, and what that was: 1 for +inf, -256 for -inf, both (-255) for NaN.  A product with ones where there is
 // weight, over 64 rows at most, says what a channel has met.

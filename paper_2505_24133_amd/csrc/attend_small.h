@@ -117,13 +117,12 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int block, Lds<MT>& 
       float x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = s[m][i >> 2][i & 3] * a.scale2;
-      if (edge) {
+      if (edge) {                                                // bit 16 (i >> 2) + (i & 3) from row start + 4 g4 on
+        const int from = start + 4 * g4;
+        const uint32_t seen = (bits_from(max(see[m].lo, base) - from) | (bits_from(base - from) & ~bits_from(sinks - from))) &
+                              ~bits_from(min(see[m].hi, span.end(t)) - from);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = start + (i >> 2) * 16 + 4 * g4 + (i & 3);
-          const bool seen = c < min(see[m].hi, span.end(t)) && c >= base && (c >= see[m].lo || c < sinks);
-          x[i] = seen ? x[i] : -INFINITY;
-        }
+        for (int i = 0; i < 8; ++i) x[i] = seen_or(x[i], seen, 16 * (i >> 2) + (i & 3));
       }
       float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
       top = fmaxf(top, __shfl_xor(top, 16));
@@ -155,7 +154,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int block, Lds<MT>& 
         const int row = vrow + half * 16, chunk = 2 * d + ((col & 3) >> 1);
         vf.s[half] = read_transposed(vt + row * kRowBytes + (value_chunk(row, chunk) << 4) + ((col & 1) << 3));
       }
-      if (edge && __any(not_finite(vf))) {
+      if (edge && __any(not_finite(largest_magnitudes(0, vf)))) {
         const Frag bad = take_not_finite(vf);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {

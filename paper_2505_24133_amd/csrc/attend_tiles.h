@@ -193,14 +193,12 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int splits, int bloc
       const bool edge = t < plain_lo || t >= plain_hi;
       if (__builtin_expect(edge, 0)) {
         asm volatile("" ::: "memory");                   // (a branch, not a selection made for every step)
-        const int start = span.start(t), stop = min(span.end(t), start + kKeys);
+        // the rows that this lane's query sees, a bit each from row start + 4 half on; element i has bit 8 (i >> 2) + (i & 3)
+        const int from = span.start(t) + 4 * half, stop = min(span.end(t), span.start(t) + kKeys);
         const Sight see = sights[wave * 32 + col];
+        const uint32_t seen = (bits_from(max(see.lo, base) - from) | (bits_from(base - from) & ~bits_from(sinks - from))) & ~bits_from(min(see.hi, stop) - from);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int c = start + 8 * (i >> 2) + 4 * half + (i & 3);
-          const bool seen = c < min(see.hi, stop) && c >= base && (c >= see.lo || c < sinks);
-          s[i] = seen ? s[i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) s[i] = seen_or(s[i], seen, 8 * (i >> 2) + (i & 3));
       }
       float top = s[0];
 #pragma unroll
@@ -248,9 +246,17 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int splits, int bloc
       __builtin_amdgcn_sched_barrier(0);
       if (__builtin_expect(edge, 0)) {
         // what is not finite is taken out of the values, and added where a weight meets it
+        bool some = false;
+        {
+          uint32_t largest = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (__any(not_finite(vf[i]))) {
+          for (int i = 0; i < 8; ++i) largest = largest_magnitudes(largest, vf[i]);
+          some = __any(not_finite(largest));
+        }
+        if (__builtin_expect(some, 0)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            __builtin_amdgcn_sched_barrier(0);           // (one fragment at a time: there are no registers for more)
             f32x16 met;
 #pragma unroll
             for (int e = 0; e < 16; ++e) met[e] = 0.f;
