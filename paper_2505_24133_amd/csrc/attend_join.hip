@@ -113,7 +113,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int rows
 }  // namespace
 
 hipError_t launch_attend_join(const AttendArgs& a, hipStream_t stream) {
-  const JoinMode mode = a.small_splits == 0 || a.small_by_token ? kTokens : (a.prefix_splits > 0 || a.tile_splits > 1 ? kMixed : kUnits);
+  // (by token alone only where every row that it reads has been written: the few-rows kernel says so of prefixes that a problem does not have)
+  const JoinMode mode = a.small_by_token || (a.small_splits == 0 && a.prefix_splits == 0) ? kTokens :
+                        (a.prefix_splits > 0 || a.tile_splits > 1 ? kMixed : kUnits);
   const int parts = a.prefix_splits + (a.small_splits > a.tile_splits || mode == kUnits ? a.small_splits : a.tile_splits);
   const int rows = mode == kUnits ? a.small_rows : a.H * a.G;
   const int64_t outer = mode == kUnits ? (int64_t)a.P * a.H : a.T;

@@ -110,6 +110,15 @@ def test_groups_in_the_middle_and_padding():
     assert bool(((out[5:5 + n].double() - want[0][:n]).abs() <= want[2][:n]).all()) and (out[:5] == 3).all() and (out[5 + n:] == 3).all()
 
 
+@pytest.mark.parametrize("G, new", [(70, [1]), (66, [2, 0, 1]), (4, [1, 30])])
+def test_problems_in_no_group_beside_many_rows(G, new):
+    """What the workspace held before is not taken for a prefix's part."""
+    b = grouped(1, G, [2], [90], new, [5, 40], outside=3, seed=11)
+    ws = rkv.make_attend_workspace(b.shape, b.T, max(b.new), groups=1)
+    for left in (0, 1, 0x3f, 0x7f, 0xff):
+        check(run(b, ws=ws.fill_(left)), attend64(b), f"workspace of {left}")
+
+
 def test_no_groups():
     b = Batch(2, 4, [1, 2], [100, 300], seed=7)
     b.group_starts, b.prefix_len = int32([0]), int32([])
