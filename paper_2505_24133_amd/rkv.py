@@ -637,10 +637,13 @@ def _attend(shape: Shape, q, k, v, starts, kv_len, group_starts, prefix_len, win
         if s != RKV_OK:
             raise RkvError(s, where)
         ws = torch.empty(n.value + 256, dtype=torch.uint8, device=q.device)
+    elif ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous uint8, got {ws.dtype} with strides {ws.stride()}")
     base = ws.data_ptr()
     aligned = (base + 255) & ~255
     call = lib.rkv_attend if group_starts is None else lib.rkv_attend_shared
-    s = call(ctypes.byref(prm), ctypes.byref(att), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), aligned, ws.numel() - (aligned - base), _stream())
+    s = call(ctypes.byref(prm), ctypes.byref(att), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), aligned,
+             max(ws.numel() - (aligned - base), 0), _stream())
     if s != RKV_OK:
         raise RkvError(s, where)
     return (out, lse) if lse is not None else out
