@@ -71,7 +71,7 @@ rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_param
  * first problem's cache; the result is rkv_attend's.  Problems in no group are attended by themselves.
  *
  * Both need a workspace of rkv_attend_workspace_size() bytes (0 for calls that need none), 256-byte aligned; the size for a window of 0 does for
- * any window.  out must not overlap the other arrays.  groups is 0 for rkv_attend.
+ * any window.  out must not overlap the other arrays, nor (refused) its rows each other.  groups is 0 for rkv_attend.
  */
 typedef struct {
   int32_t tokens;            /* T >= 0 */

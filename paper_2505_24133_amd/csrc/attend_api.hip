@@ -53,11 +53,16 @@ rkv_status read_caches(const rkv_params& q, int num_pages, Caches* c) {
   return RKV_OK;
 }
 
-// Strides of an array [T, heads, d]; 0, 0 = dense.
-bool token_strides(int64_t st, int64_t sh, int heads, int64_t tokens, int64_t* ot, int64_t* oh) {
+// Strides of an array [T, heads, d]; 0, 0 = dense.  Rows that are written must not lie in each other: one kind of stride is at least a
+// row, the other one at least all of its rows.
+bool token_strides(int64_t st, int64_t sh, int heads, int64_t tokens, int64_t* ot, int64_t* oh, bool written) {
   if (st == 0 && sh == 0) { *oh = kHeadDim; *ot = (int64_t)heads * kHeadDim; return true; }
   *ot = st; *oh = sh;
-  return wide_stride(st, tokens > 1) && wide_stride(sh, heads > 1) && st <= (int64_t)1 << 40 && sh <= (int64_t)1 << 40;
+  if (!wide_stride(st, tokens > 1) || !wide_stride(sh, heads > 1) || st > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return false;
+  if (!written) return true;
+  if ((heads > 1 && sh < kHeadDim) || (tokens > 1 && st < kHeadDim)) return false;
+  // (divided, for the product of the second could pass 64 bits)
+  return heads <= 1 || tokens <= 1 || st >= (heads - 1) * sh + kHeadDim || (sh - kHeadDim) / (tokens - 1) >= st;
 }
 
 struct AttendPlan {
@@ -111,8 +116,8 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   if (t.window < 0 || t.sinks < 0 || !(t.scale > 0.f) || !isfinite(t.scale)) return RKV_ERR_PARAM;
   AttendArgs& a = pl->a;
   a = AttendArgs{};
-  if (!token_strides(t.q_stride_token, t.q_stride_head, c.H * c.G, t.tokens, &a.qst, &a.qsh) ||
-      !token_strides(t.o_stride_token, t.o_stride_head, c.H * c.G, t.tokens, &a.ost, &a.osh))
+  if (!token_strides(t.q_stride_token, t.q_stride_head, c.H * c.G, t.tokens, &a.qst, &a.qsh, false) ||
+      !token_strides(t.o_stride_token, t.o_stride_head, c.H * c.G, t.tokens, &a.ost, &a.osh, true))
     return RKV_ERR_SHAPE;
   a.starts = t.starts; a.kv_len = t.kv_len; a.group_starts = t.group_starts; a.prefix_len = t.prefix_len;
   a.P = c.P; a.H = c.H; a.G = c.G; a.N = c.N; a.T = t.tokens; a.groups = t.groups;
@@ -233,10 +238,10 @@ rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_param
   if (r.tokens > kMaxTokens / 2 || r.rotary_dim < 16 || r.rotary_dim > kHeadDim || r.rotary_dim % 16 != 0) return RKV_ERR_UNSUPPORTED;
   if (r.interleaved != 0 && r.interleaved != 1) return RKV_ERR_PARAM;
   RotaryArgs a = {};
-  if (!token_strides(r.k_stride_token, r.k_stride_head, c.H, r.tokens, &a.knt, &a.knh) ||
-      !token_strides(r.v_stride_token, r.v_stride_head, c.H, r.tokens, &a.vnt, &a.vnh) ||
-      !token_strides(r.q_stride_token, r.q_stride_head, Hq, r.tokens, &a.qnt, &a.qnh) ||
-      !token_strides(r.o_stride_token, r.o_stride_head, Hq, r.tokens, &a.qot, &a.qoh))
+  if (!token_strides(r.k_stride_token, r.k_stride_head, c.H, r.tokens, &a.knt, &a.knh, false) ||
+      !token_strides(r.v_stride_token, r.v_stride_head, c.H, r.tokens, &a.vnt, &a.vnh, false) ||
+      !token_strides(r.q_stride_token, r.q_stride_head, Hq, r.tokens, &a.qnt, &a.qnh, false) ||
+      !token_strides(r.o_stride_token, r.o_stride_head, Hq, r.tokens, &a.qot, &a.qoh, true))
     return RKV_ERR_SHAPE;
   a.alpha = 1;
   if (q_cache != nullptr) {

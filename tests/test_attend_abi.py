@@ -227,3 +227,17 @@ def test_rotary_tables_at_far_positions():
     for i in range(8):
         angle = 1000000 * 500000.0 ** (-2 * i / 16)
         assert abs(cos[-1, i].item() - math.cos(angle)) < 1e-7 and abs(sin[-1, i].item() - math.sin(angle)) < 1e-7
+
+
+def test_outputs_whose_rows_lie_in_each_other_are_refused(lib):
+    p = block(shape())                                                     # 2 problems, 32 query heads
+    for st, sh, tokens, good in ((4096, 128, 5, True), (128, 5 * 128, 5, True), (4096 + 64, 128, 5, True), (4096 - 8, 128, 5, False),
+                                 (4096, 64, 5, False), (64, 4096, 5, False), (128, 4 * 128, 5, False), (128, 5 * 128 - 8, 5, False),
+                                 (0, 128, 1, True), (8, 128, 1, True), (0, 64, 1, False), (1 << 40, 128, 1 << 20, True),
+                                 (1 << 40, 1 << 40, 1 << 24, False), (128, 1 << 40, 1 << 24, True)):
+        want = rkv.RKV_OK if good else rkv.RKV_ERR_SHAPE
+        one_each = dict(tokens=tokens, max_new=1)
+        got = size(lib, p, att(o_stride_token=st, o_stride_head=sh, **one_each))[0]
+        assert got == want or (good and got == rkv.RKV_ERR_UNSUPPORTED), (st, sh, tokens)
+        # queries may lie in each other
+        assert size(lib, p, att(q_stride_token=max(st, 8), q_stride_head=sh, **one_each))[0] != rkv.RKV_ERR_SHAPE

@@ -40,3 +40,86 @@ def test_workspaces_that_do_not_do(path):
             call(other)
     check(call(room), attend64(b))
     check(call(room[1:]), attend64(b))
+
+
+def rotary_call(b, interleaved, q_out=None):
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    wide = torch.randn((b.T, b.H * (b.G + 2), 128), generator=gen, device="cuda").bfloat16()
+    q, k, v = wide[:, :b.H * b.G], wide[:, b.H * b.G:b.H * (b.G + 1)], wide[:, b.H * (b.G + 1):]
+    cos, sin = rkv.rotary_tables(500, 64)
+    ring = torch.zeros((b.P, b.H * b.G, b.shape.alpha, 128), dtype=torch.bfloat16, device="cuda")
+    held = b.kv_len - (b.starts[1:] - b.starts[:-1])
+    keys, values = b.k.clone(), b.v.clone()
+    got = rkv.rkv_cache_append_rotary(b.shape, keys, values, ring, k, v, q, cos, sin, b.starts, held, held + 3, interleaved=interleaved, q_out=q_out)
+    return got, ring, keys, values
+
+
+@pytest.mark.parametrize("how", [dict(), dict(strided=True), dict(page=32)])
+def test_both_paths_give_the_same_bytes(how, monkeypatch):
+    print(f"[gpu-case] both paths {how}", flush=True)
+    rkv.load_library()
+    b = Batch(2, 3, [1, 0, 4], [200, 70, 90], seed=2, **how)
+    first, lens = int32([1, 3]), int32([32])
+    ws = rkv.make_attend_workspace(b.shape, b.T, 4, groups=1)
+    b.rows_k[2, :, :32], b.rows_v[2, :, :32] = b.rows_k[1, :, :32], b.rows_v[1, :, :32]
+    b.store()
+
+    def everything():
+        got = [*rotary_call(b, False), *rotary_call(b, True, torch.empty((b.T, 6, 128), dtype=torch.bfloat16, device="cuda"))]
+        for kw in (dict(), dict(window=20, sinks=3), dict(scale=0.2), dict(out=torch.empty((b.T, 9, 128), dtype=torch.bfloat16, device="cuda")[:, 2:8])):
+            lists = b.shape, b.q, b.k, b.v, b.starts, b.kv_len
+            got += [*rkv.rkv_attend(*lists, max_new=4, want_lse=True, ws=ws, **kw), *rkv.rkv_attend_shared(*lists, first, lens, max_new=4, want_lse=True, ws=ws, **kw)]
+            got.append(rkv.rkv_attend(*lists, ws=rkv.make_attend_workspace(b.shape, b.T), **kw))
+            kw.pop("out", None)
+            got.append(rkv.rkv_attend(*lists, **kw))
+        return [t.clone() for t in got]
+
+    native = everything()
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        aside = everything()
+    other.synchronize()
+    monkeypatch.setattr(rkv, "_append_rotary", lambda *args: None)
+    monkeypatch.setattr(rkv, "_attend_native", lambda *args: None)
+    for got in (aside, everything()):
+        assert len(got) == len(native)
+        for i, (x, y) in enumerate(zip(native, got)):
+            assert torch.equal(x, y), i
+
+
+def test_what_the_binding_refuses(path):
+    b = Batch(2, 3, [1, 2], [50, 60], seed=3)
+    half = b.q.half()
+    lists = [b.shape, b.q, b.k, b.v, b.starts, b.kv_len]
+
+    def refused(error, i=None, value=None, match=None, **kw):
+        args = list(lists)
+        if i is not None:
+            args[i] = value
+        with pytest.raises(error, match=match):
+            rkv.rkv_attend(*args, **kw)
+
+    refused(RuntimeError, 1, b.q.cpu())
+    refused(ValueError, 1, half, "q must be")
+    refused(ValueError, 1, b.q[:, :5], "q must be")
+    refused(ValueError, 1, b.q.transpose(1, 2).contiguous().transpose(1, 2), "q must be")
+    refused(ValueError, 2, b.k[:1])
+    refused(ValueError, 4, b.starts[:2], "starts must be")
+    refused(ValueError, 4, b.starts.long(), "starts must be")
+    refused(ValueError, 5, torch.zeros((2, 2), dtype=torch.int32, device="cuda")[:, 0], "kv_len must be")
+    refused(ValueError, window=-1, match="window, sinks")
+    refused(ValueError, sinks=2 ** 31, match="window, sinks")
+    refused(ValueError, out=b.q[:2], match="out must be")
+    refused(ValueError, lse=torch.empty((3, 5), device="cuda"), match="lse must be")
+    refused(rkv.RkvError, max_new=4, match="status -2")
+    refused(rkv.RkvError, max_new=0, match="status -2")
+    for scale in (0.0, float("inf"), -1.0):
+        refused(rkv.RkvError, scale=scale)
+    # rows of the outputs that lie in each other
+    room = torch.zeros(3 * 6 * 128, dtype=torch.bfloat16, device="cuda")
+    for strides in ((6 * 128, 64, 1), (64, 128 * 3, 1)):
+        refused(rkv.RkvError, out=room.as_strided((3, 6, 128), strides), match="status -2")
+    with pytest.raises(ValueError, match="group_starts must be"):
+        rkv.rkv_attend_shared(*lists, int32([0, 1]), int32([1, 2]))
+    check(rkv.rkv_attend(*lists, want_lse=True), attend64(b))
