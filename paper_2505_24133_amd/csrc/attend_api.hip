@@ -138,6 +138,8 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   if (small) {
     a.small_rows = large || most_rows > 32 ? 64 : (most_rows > 16 ? 32 : 16);
     split_small((int64_t)c.P * c.H, reach, &a);
+    // (a workgroup a row, which the join takes for more than 32 parts, would be more threads than a launch has)
+    if (rows > (1 << 22)) a.small_splits = std::min(a.small_splits, 30);
     // (a token array that is mostly padding would make for large parts by token)
     a.small_by_token = !large && rows <= (int64_t)c.P * c.H * a.small_rows;
   }
@@ -145,7 +147,7 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   if (t.groups > 0) a.prefix_splits = split_tiles(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, rows, reach, c.N);
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
-      (int64_t)t.tokens * ((c.H * c.G + 7) / 8) > kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)
+      (int64_t)t.tokens * ((c.H * c.G + 7) / 8) >= kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)
     return RKV_ERR_UNSUPPORTED;
 
   auto take = [&](int64_t bytes) {

@@ -307,7 +307,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int splits, int bloc
     else if (a.lse != nullptr) a.lse[at] = lse_of(mx, sum);
   }
   if (!whole && t_lo == t_hi) return;                    // (of a part without rows -inf, 0 is all that is read)
-  asm volatile("s_barrier" ::: "memory");
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kHeadDim;
   const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
 #pragma unroll
