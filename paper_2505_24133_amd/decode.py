@@ -36,7 +36,8 @@ class DecodeCache:
         self.compressions = 0
         self._counts = None        # row n: n for every problem (what the calls take as lengths), made at the first step
         self._starts = {}          # by new tokens a problem: where each problem's begin
-        self._attend_ws = {}       # and the workspace of their attention
+        self._attend_room = {}     # and how much workspace their attention needs; one workspace serves them all
+        self._attend_ws = None
         self._groups = None
 
     @property
@@ -68,14 +69,15 @@ class DecodeCache:
         rows[1], ... (samples of one prompt): step() reads those rows once for all of them, until the first compression, after
         which every problem has rows of its own."""
         sizes, rows = [int(n) for n in group_sizes], [int(n) for n in rows]
-        if len(sizes) != len(rows) or min(sizes + rows, default=0) < 0 or sum(sizes) > self.shape.num_problems or max(rows, default=0) > self.length:
+        P = self.shape.num_problems
+        if len(sizes) != len(rows) or len(sizes) > P or min(sizes + rows, default=0) < 0 or sum(sizes) > P or max(rows, default=0) > self.length:
             raise ValueError("share_prompt needs as many row counts as groups, groups of the problems there are and rows that are held")
         first = [0]
         for n in sizes:
             first.append(first[-1] + n)
         device = self.q_cache.device
         self._groups = (torch.tensor(first, dtype=torch.int32, device=device), torch.tensor(rows, dtype=torch.int32, device=device)) if sizes else None
-        self._attend_ws = {}
+        self._attend_room = {}
 
     def step(self, q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor,
              interleaved: bool = False, window: int = 0, sinks: int = 0, scale=None) -> torch.Tensor:
@@ -94,22 +96,24 @@ class DecodeCache:
             self._counts = torch.arange(s.n_tokens + 1, dtype=torch.int32, device=device)[:, None].expand(-1, P).contiguous()
         if n not in self._starts:
             self._starts[n] = torch.arange(0, P * n + 1, n, dtype=torch.int32, device=self.q_cache.device)
-        if n not in self._attend_ws:
-            groups = 0 if self._groups is None else self._groups[1].shape[0]
-            self._attend_ws[n] = rkv.make_attend_workspace(s, P * n, n, groups, self.q_cache.device)
+        if n not in self._attend_room:
+            self._attend_room[n] = rkv.rkv_attend_workspace_size(s, P * n, n, 0 if self._groups is None else self._groups[1].shape[0])
+        if self._attend_ws is None or self._attend_ws.numel() < self._attend_room[n] + 256:
+            self._attend_ws = torch.empty(self._attend_room[n] + 256, dtype=torch.uint8, device=self.q_cache.device)
         starts, k, v = self._starts[n], self.k, self.v
         # positions count from the last multiple of alpha, whose rows of the tables come first: the slots of the query cache go by them
         slot = self.tokens_seen % s.alpha
         at = self.tokens_seen - slot
         q = rkv.rkv_cache_append_rotary(s, k, v, self.q_cache, k_new.flatten(0, 1), v_new.flatten(0, 1), q_new.flatten(0, 1), cos[at:], sin[at:],
                                         starts, self._counts[self.length], self._counts[slot], interleaved=interleaved)
-        self.length += n
-        self.tokens_seen += n
-        common = dict(window=window, sinks=sinks, scale=scale, max_new=n, ws=self._attend_ws[n])
+        lens = self._counts[self.length + n]
+        common = dict(window=window, sinks=sinks, scale=scale, max_new=n, ws=self._attend_ws)
         if self._groups is None:
-            out = rkv.rkv_attend(s, q, k, v, starts, self._counts[self.length], **common)
+            out = rkv.rkv_attend(s, q, k, v, starts, lens, **common)
         else:
-            out = rkv.rkv_attend_shared(s, q, k, v, starts, self._counts[self.length], *self._groups, **common)
+            out = rkv.rkv_attend_shared(s, q, k, v, starts, lens, *self._groups, **common)
+        self.length += n                                   # (a step that was refused has not taken place)
+        self.tokens_seen += n
         if self.length >= s.n_tokens > s.budget:
             self.compress()
         return out.view(P, n, s.q_heads, s.head_dim)
@@ -118,7 +122,8 @@ class DecodeCache:
         s = self.shape
         if self.length != s.n_tokens:
             raise RuntimeError("compress() runs when the cache holds budget + buffer rows")
-        self._groups, self._attend_ws = None, self._attend_ws if self._groups is None else {}
+        if self._groups is not None:
+            self._groups, self._attend_room = None, {}
         if self.inplace:
             st, *_ = rkv.rkv_compress_inplace(s, self.q_cache, self.k, self.v, ws=self._ws, kept_idx=self.kept_idx)
             if st != rkv.RKV_OK:

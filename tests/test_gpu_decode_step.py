@@ -78,3 +78,33 @@ def test_refusals():
     for sizes, rows in (([2], [5]), ([1], [21]), ([1], [5, 6]), ([-1], [3])):
         with pytest.raises(ValueError, match="share_prompt"):
             cache.share_prompt(sizes, rows)
+
+
+def test_a_refused_step_has_not_taken_place():
+    s = shape(2, 1, 2, 40, 30)
+    cos, sin = rkv.rotary_tables(200)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    tokens = [tuple(torch.randn((2, n, h, 128), generator=gen, device="cuda").bfloat16() for h in (2, 1, 1)) for n in (9, 1, 3)]
+    straight, stumbling = decode.DecodeCache(s), decode.DecodeCache(s)
+    for t in tokens:
+        want = straight.step(*t, cos, sin)
+        for error, kw in ((ValueError, dict(window=-1)), (rkv.RkvError, dict(scale=0.0))):
+            held = stumbling.length, stumbling.tokens_seen
+            with pytest.raises(error):
+                stumbling.step(*t, cos, sin, **kw)
+            assert (stumbling.length, stumbling.tokens_seen) == held
+        assert torch.equal(stumbling.step(*t, cos, sin), want)
+    assert torch.equal(stumbling.k, straight.k) and torch.equal(stumbling.v, straight.v) and torch.equal(stumbling.q_cache, straight.q_cache)
+    with pytest.raises(ValueError, match="share_prompt"):
+        straight.share_prompt([0, 0, 0], [1, 1, 1])
+
+
+def test_one_workspace_for_all_lengths():
+    s = shape(1, 1, 4, 4000, 3000)
+    cache = decode.DecodeCache(s)
+    cos, sin = rkv.rotary_tables(4000)
+    at_most = max(rkv.rkv_attend_workspace_size(s, n, n) for n in range(1, 60)) + 256
+    for n in (3, 50, 1, 40, 2, 33):
+        t = [torch.zeros((1, n, h, 128), dtype=torch.bfloat16, device="cuda") for h in (4, 1, 1)]
+        cache.step(*t, cos, sin)
+        assert cache._attend_ws.numel() <= at_most
