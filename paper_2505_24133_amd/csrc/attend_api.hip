@@ -68,6 +68,7 @@ bool token_strides(int64_t st, int64_t sh, int heads, int64_t tokens, int64_t* o
 struct AttendPlan {
   AttendArgs a;
   bool paged;
+  bool fused;                  // shared prefixes and few-rows units in one launch
   size_t off_small_o, off_small_ml, off_tile_o, off_tile_ml, off_prefix_o, off_prefix_ml, total;
 };
 
@@ -104,6 +105,29 @@ int split_tiles(int64_t tiles, int64_t rows, int64_t reach, int64_t all) {
   return reach == all ? s : std::min(s, split_tiles(tiles, rows, all));
 }
 
+// Shared prefixes in one launch with the few-rows units behind them: a prefix's workgroup is a chain of dependent steps (0.55 us each, 5 for the
+// start), which costs nothing as long as the units (10 us for 512 of them) and the steps of all workgroups keep the chip busy (0.4 us for
+// 512 of them, and eight for each start); every part is written and read again (0.45 us for 1000 rows of queries).  Fitted to 17 sizes, where
+// it picks what is 3 % slower than the best on average.  64 samples of 8 KV heads behind 4099 rows: 6 parts 32.6 us, 2 parts 56.5, 16
+// parts 36.6; behind 16000 rows 13 parts 46, 6 parts 71, 32 parts 55; 32 times 2 samples behind 1000 rows 1 part 35, 4 parts 43; 16
+// samples behind 8000 rows 32 parts 22.1, 6 parts 40.
+int split_prefix(int64_t tiles, int64_t rows, int64_t reach, int64_t units) {
+  const int64_t steps = (reach + 31) / 32;
+  const double busy = 5.0 + 10.0 * (double)std::min(units, kSlots) / (double)kSlots;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 32 && (s == 1 || s * 4 <= steps); ++s) {
+    const double chain = 5.0 + 0.55 * (double)((steps + s - 1) / s), work = 0.4 * (double)tiles * (double)(steps + 8 * s) / (double)kSlots;
+    const double cost = std::max(chain, busy + work) + 0.45e-3 * (double)rows * s;
+    if (s == 1 || cost < least) { best = s; least = cost; }
+  }
+  return best;
+}
+int split_prefix(int64_t tiles, int64_t rows, int64_t reach, int64_t units, int64_t all) {
+  const int s = split_prefix(tiles, rows, reach, units);
+  return reach == all ? s : std::min(s, split_prefix(tiles, rows, all, units));
+}
+
 rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool shared, AttendPlan* pl) {
   if (prm == nullptr || att == nullptr) return RKV_ERR_NULL;
   const rkv_attend_params& t = *att;
@@ -126,6 +150,7 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   a.scale2 = t.scale * 1.4426950408889634f;
   pl->paged = c.paged;
   pl->total = 0;
+  pl->fused = false;
   if (c.P == 0 || t.tokens == 0) return RKV_OK;
 
   // Which kernels run.  Up to 64 rows of queries per KV head (new tokens * G) the few-rows kernel has them; where a problem may have
@@ -144,7 +169,11 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
     a.small_by_token = !large && rows <= (int64_t)c.P * c.H * a.small_rows;
   }
   if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach, c.N);
-  if (t.groups > 0) a.prefix_splits = split_tiles(attend_tile_bound(t.tokens, c.G, t.groups) * c.H, rows, reach, c.N);
+  if (t.groups > 0) {
+    const int64_t tiles = attend_tile_bound(t.tokens, c.G, t.groups) * c.H;
+    pl->fused = !large && a.small_rows <= 32;
+    a.prefix_splits = pl->fused ? split_prefix(tiles, rows, reach, (int64_t)c.P * c.H, c.N) : split_tiles(tiles, rows, reach, c.N);
+  }
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
       (int64_t)t.tokens * ((c.H * c.G + 7) / 8) >= kMaxBlocks * 2 || (int64_t)c.P * c.H * 8 > kMaxBlocks * 4)
@@ -192,7 +221,7 @@ rkv_status attend(const rkv_params* prm, const rkv_attend_params* att, bool shar
   a.prefix_o = reinterpret_cast<float*>(w + pl.off_prefix_o);
   a.prefix_ml = reinterpret_cast<float2*>(w + pl.off_prefix_ml);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (a.prefix_splits > 0 && a.tile_splits == 0 && a.small_rows <= 32) {
+  if (pl.fused) {
     if (launch_attend_prefix(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
   } else {
     if (a.prefix_splits > 0 && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
