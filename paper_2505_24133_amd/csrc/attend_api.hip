@@ -72,14 +72,16 @@ struct AttendPlan {
   size_t off_small_o, off_small_ml, off_tile_o, off_tile_ml, off_prefix_o, off_prefix_ml, total;
 };
 
-// Into how many workgroups the rows of a few-rows unit are dealt, at most, and how many rows are worth one: as many as the chip takes at
-// once, with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out (not behind
-// shared prefixes: what is left of the rows there is not known here, and workgroups that find nothing to do are not free: 64 samples of
-// one prompt 4 us).  48 ragged caches of up to 8320 rows under a window of 4096: 174 us with one workgroup a unit, 150 with four.
+// Into how many workgroups the rows of a few-rows unit are dealt, at most, and how many rows are worth one: as many as the chip takes at once,
+// with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out (not behind shared
+// prefixes: what is left of the rows there is not known here, and workgroups that find nothing to do are not free: 64 samples of one prompt 4
+// us), and one workgroup where the join would cost more than the rows: 101 rows of one sequence, 8 KV heads, 6.3 us whole and 8.1 in two
+// parts, 501 rows 13.3 and 8.3; 301 rows of 16 sequences 10.1 and 11.5 (not with up to 64 rows of queries: 13.9 in parts, 15.4 whole).  48
+// ragged caches of up to 8320 rows under a window of 4096: 174 us with one workgroup a unit, 150 with four.
 void split_small(int64_t units, int64_t reach, AttendArgs* a) {
   const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + 63) / 64);
   const int64_t even = a->groups > 0 ? 0 : std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
-  a->small_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
+  a->small_splits = a->groups == 0 && a->small_rows <= 32 && reach <= 192 + units ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
   a->small_share = fill >= even ? 64 : 512;
 }
 
