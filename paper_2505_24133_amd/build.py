@@ -15,7 +15,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librkv.so")
 HOST = os.path.join(HERE, "_host" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.hip", "prepass.hip", "gram.hip", "gram_few.hip", "finalize.hip", "gather.hip", "compact_inplace.hip", "append.hip", "probe.hip",
-           "append_rotary.hip", "attend_small.hip", "attend_tiles.hip", "attend_prefix.hip", "attend_join.hip", "attend_api.hip"]
+           "append_rotary.hip", "attend_small.hip", "attend_tiles.hip", "attend_beside.hip", "attend_join.hip", "attend_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

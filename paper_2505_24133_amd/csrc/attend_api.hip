@@ -68,7 +68,6 @@ bool token_strides(int64_t st, int64_t sh, int heads, int64_t tokens, int64_t* o
 struct AttendPlan {
   AttendArgs a;
   bool paged;
-  bool fused;                  // shared prefixes and few-rows units in one launch
   size_t off_small_o, off_small_ml, off_tile_o, off_tile_ml, off_prefix_o, off_prefix_ml, total;
 };
 
@@ -76,12 +75,12 @@ struct AttendPlan {
 // with 64 rows each, then more where a unit still has 1024 rows for each, so that units of different lengths even out (not behind shared
 // prefixes: what is left of the rows there is not known here, and workgroups that find nothing to do are not free: 64 samples of one prompt 4
 // us), and one workgroup where the join would cost more than the rows: 101 rows of one sequence, 8 KV heads, 6.3 us whole and 8.1 in two
-// parts, 501 rows 13.3 and 8.3; 301 rows of 16 sequences 10.1 and 11.5 (not with up to 64 rows of queries: 13.9 in parts, 15.4 whole).  48
+// parts, 501 rows 13.3 and 8.3; 301 rows of 16 sequences 10.1 and 11.5.  48
 // ragged caches of up to 8320 rows under a window of 4096: 174 us with one workgroup a unit, 150 with four.
 void split_small(int64_t units, int64_t reach, AttendArgs* a) {
   const int64_t fill = std::min((kSmallSlots + units - 1) / units, (reach + 63) / 64);
   const int64_t even = a->groups > 0 ? 0 : std::min((4 * kSmallSlots + units - 1) / units, reach / 1024);
-  a->small_splits = a->groups == 0 && a->small_rows <= 32 && reach <= 192 + units ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
+  a->small_splits = a->groups == 0 && reach <= 192 + units ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), kMaxSplits));
   a->small_share = fill >= even ? 64 : 512;
 }
 
@@ -152,18 +151,21 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   a.scale2 = t.scale * 1.4426950408889634f;
   pl->paged = c.paged;
   pl->total = 0;
-  pl->fused = false;
   if (c.P == 0 || t.tokens == 0) return RKV_OK;
 
-  // Which kernels run.  Up to 64 rows of queries per KV head (new tokens * G) the few-rows kernel has them; where a problem may have
-  // more, the many-rows kernel has those problems, and the few-rows kernel the others if there are any.
+  // Which kernels run.  Up to 32 rows of queries per KV head (new tokens * G) the few-rows kernel has them; where a problem may have
+  // more, the many-rows kernel has those problems, and the few-rows kernel the others if there are any, in the same launch.  (A few-rows
+  // kernel for up to 64 rows lost: 16 tokens of 4 heads behind 1000 rows 17.1 us, in tiles 12.8, behind 8000 rows of 4 sequences 45.6 and
+  // 37.3; only many sequences of very different lengths were 4 to 13 % faster with it.)
   const int64_t most_rows = (int64_t)t.max_new * c.G, rows = (int64_t)t.tokens * c.H * c.G;
   const bool large = most_rows > kSmallRows;
-  const bool small = !large || (c.P > 1 && c.G <= kSmallRows);
+  // (where a problem with so few would leave the others more than max_new each there is none, unless tokens are padding: the many-rows
+  // kernel has it then)
+  const bool small = !large || (c.P > 1 && c.G <= kSmallRows && (int64_t)t.tokens * c.G - (int64_t)(c.P - 1) * most_rows <= kSmallRows);
   // rows that a query may see, at most
   const int64_t reach = t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + t.max_new) : c.N;
   if (small) {
-    a.small_rows = large || most_rows > 32 ? 64 : (most_rows > 16 ? 32 : 16);
+    a.small_rows = large || most_rows > 16 ? 32 : 16;
     split_small((int64_t)c.P * c.H, reach, &a);
     // (a workgroup a row, which the join takes for more than 32 parts, would be more threads than a launch has)
     if (rows > (1 << 22)) a.small_splits = std::min(a.small_splits, 30);
@@ -173,8 +175,7 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach, c.N);
   if (t.groups > 0) {
     const int64_t tiles = attend_tile_bound(t.tokens, c.G, t.groups) * c.H;
-    pl->fused = !large && a.small_rows <= 32;
-    a.prefix_splits = pl->fused ? split_prefix(tiles, rows, reach, (int64_t)c.P * c.H, c.N) : split_tiles(tiles, rows, reach, c.N);
+    a.prefix_splits = !large ? split_prefix(tiles, rows, reach, (int64_t)c.P * c.H, c.N) : split_tiles(tiles, rows, reach, c.N);
   }
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
@@ -223,13 +224,12 @@ rkv_status attend(const rkv_params* prm, const rkv_attend_params* att, bool shar
   a.prefix_o = reinterpret_cast<float*>(w + pl.off_prefix_o);
   a.prefix_ml = reinterpret_cast<float2*>(w + pl.off_prefix_ml);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (pl.fused) {
-    if (launch_attend_prefix(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
-  } else {
-    if (a.prefix_splits > 0 && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
-    if (a.tile_splits > 0 && launch_attend_tiles(a, pl.paged, false, st) != hipSuccess) return RKV_ERR_HIP;
-    if (a.small_splits > 0 && launch_attend_small(a, pl.paged, st) != hipSuccess) return RKV_ERR_HIP;
-  }
+  const bool prefix_beside = a.prefix_splits > 0 && a.tile_splits == 0;      // (there are few-rows units then)
+  if (a.prefix_splits > 0 && !prefix_beside && launch_attend_tiles(a, pl.paged, true, st) != hipSuccess) return RKV_ERR_HIP;
+  const hipError_t own = prefix_beside ? launch_attend_beside(a, pl.paged, true, st) :
+                         a.tile_splits == 0 ? launch_attend_small(a, pl.paged, st) :
+                         a.small_splits == 0 ? launch_attend_tiles(a, pl.paged, false, st) : launch_attend_beside(a, pl.paged, false, st);
+  if (own != hipSuccess) return RKV_ERR_HIP;
   if ((a.prefix_splits > 0 || a.tile_splits > 1 || a.small_splits > 1) && launch_attend_join(a, st) != hipSuccess) return RKV_ERR_HIP;
   return RKV_OK;
 }

@@ -16,7 +16,7 @@ namespace rkv {
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 
-constexpr int kSmallRows = 64;       // query rows per KV head (new tokens * G) that the kernel for few rows takes at most
+constexpr int kSmallRows = 32;       // query rows per KV head (new tokens * G) that the kernel for few rows takes at most
 constexpr int kTileRows = 128;       // query rows of a tile of the kernel for many
 
 struct AttendArgs {
@@ -35,7 +35,7 @@ struct AttendArgs {
   float scale2;                // scale * log2(e)
   // Parts of the rows, unnormalised, [split][t][hq]; those of the few-rows kernel without small_by_token [p][split][h][small_rows]
   int small_splits, tile_splits, prefix_splits;   // 0: the kernel does not run
-  int small_rows;              // most query rows of a unit of the few-rows kernel: 16, 32 or 64
+  int small_rows;              // most query rows of a unit of the few-rows kernel: 16 or 32
   bool small_by_token;
   int small_share;             // rows of the cache that are worth a workgroup of it
   float* small_o;
@@ -275,8 +275,8 @@ __device__ __forceinline__ uint2 pack4(float x, float y, float z, float w) {
 
 hipError_t launch_attend_small(const AttendArgs& a, bool paged, hipStream_t stream);
 hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool prefix, hipStream_t stream);
-// Prefixes and few-rows parts in one launch (small_rows <= 32).
-hipError_t launch_attend_prefix(const AttendArgs& a, bool paged, hipStream_t stream);
+// Tiles (of prefixes, or of problems' own rows) and few-rows units in one launch.
+hipError_t launch_attend_beside(const AttendArgs& a, bool paged, bool prefix, hipStream_t stream);
 hipError_t launch_attend_join(const AttendArgs& a, hipStream_t stream);
 
 struct RotaryArgs {

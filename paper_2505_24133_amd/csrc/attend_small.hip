@@ -17,8 +17,7 @@ hipError_t launch_attend_small(const AttendArgs& a, bool paged, hipStream_t stre
   const dim3 grid((unsigned)((int64_t)a.P * a.H * a.small_splits));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(small::kThreads), 0, stream, a); };
   if (a.small_rows <= 16) paged ? go(attend_small_kernel<1, true>) : go(attend_small_kernel<1, false>);
-  else if (a.small_rows <= 32) paged ? go(attend_small_kernel<2, true>) : go(attend_small_kernel<2, false>);
-  else paged ? go(attend_small_kernel<4, true>) : go(attend_small_kernel<4, false>);
+  else paged ? go(attend_small_kernel<2, true>) : go(attend_small_kernel<2, false>);
   return hipGetLastError();
 }
 
