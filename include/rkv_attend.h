@@ -63,8 +63,8 @@ rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_param
  * -infinity.  What a token does not see has no influence on it, infinities and NaN included.  Sums and the softmax are held in fp32; the
  * weights are rounded to bf16 before they are multiplied with v.
  *
- * max_new bounds the new tokens of one problem; the outputs of a problem that has more are unspecified.  The closer it is the better: up
- * to 32 rows of queries per KV head (max_new * G) a kernel for few rows runs alone.  T is always a valid bound.
+ * max_new bounds the new tokens of one problem; the outputs of a problem that has more are unspecified.  The closer it is the better: which
+ * kernels run, and in how many parts, goes by it.  T is always a valid bound.
  *
  * rkv_attend_shared: the problems group_starts[g] .. group_starts[g + 1] - 1 (device, int32 [groups + 1], ascending) hold the same values in
  * rows 0 .. prefix_len[g] - 1 (a prompt that they share: copies, or the same pages).  Those rows are read once for the whole group, from its

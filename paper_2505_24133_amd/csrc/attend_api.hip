@@ -158,14 +158,18 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   // kernel for up to 64 rows lost: 16 tokens of 4 heads behind 1000 rows 17.1 us, in tiles 12.8, behind 8000 rows of 4 sequences 45.6 and
   // 37.3; only many sequences of very different lengths were 4 to 13 % faster with it.)
   const int64_t most_rows = (int64_t)t.max_new * c.G, rows = (int64_t)t.tokens * c.H * c.G;
-  const bool large = most_rows > kSmallRows;
+  // 17 to 32 rows over caches that keep the chip busy are the many-rows kernel's too (whatever the window, so that its workspace does for
+  // all): three tokens of 8 heads behind 20 000 rows of 8 sequences 154 us, in tiles 127, 32 heads behind 4000 of 32 sequences 129 and 116;
+  // behind 1000 rows of 64 sequences 46 and 47, behind prefixes 33 and 46.
+  const bool heavy = most_rows > 16 && t.groups == 0 && (int64_t)c.P * c.H * c.N >= 900000;
+  const bool large = most_rows > kSmallRows || heavy;
   // (where a problem with so few would leave the others more than max_new each there is none, unless tokens are padding: the many-rows
   // kernel has it then)
   const bool small = !large || (c.P > 1 && c.G <= kSmallRows && (int64_t)t.tokens * c.G - (int64_t)(c.P - 1) * most_rows <= kSmallRows);
   // rows that a query may see, at most
   const int64_t reach = t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + t.max_new) : c.N;
   if (small) {
-    a.small_rows = large || most_rows > 16 ? 32 : 16;
+    a.small_rows = most_rows <= 16 || (heavy && most_rows <= kSmallRows) ? 16 : kSmallRows;
     split_small((int64_t)c.P * c.H, reach, &a);
     // (a workgroup a row, which the join takes for more than 32 parts, would be more threads than a launch has)
     if (rows > (1 << 22)) a.small_splits = std::min(a.small_splits, 30);

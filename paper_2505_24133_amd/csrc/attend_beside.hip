@@ -33,7 +33,8 @@ hipError_t launch_attend_beside(const AttendArgs& a, bool paged, bool prefix, hi
   const int64_t first = attend_tile_bound(a.T, a.G, prefix ? a.groups : a.P) * a.H * splits;
   const dim3 grid((unsigned)(first + (int64_t)a.P * a.H * a.small_splits));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(tiles::kThreads), 0, stream, a, splits, (int)first); };
-  if (!prefix) paged ? go(attend_beside_kernel<2, true, false>) : go(attend_beside_kernel<2, false, false>);
+  if (!prefix && a.small_rows <= 16) paged ? go(attend_beside_kernel<1, true, false>) : go(attend_beside_kernel<1, false, false>);
+  else if (!prefix) paged ? go(attend_beside_kernel<2, true, false>) : go(attend_beside_kernel<2, false, false>);
   else if (a.small_rows <= 16) paged ? go(attend_beside_kernel<1, true, true>) : go(attend_beside_kernel<1, false, true>);
   else paged ? go(attend_beside_kernel<2, true, true>) : go(attend_beside_kernel<2, false, true>);
   return hipGetLastError();

@@ -38,7 +38,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int block, Lds<MT>& 
   const int p = unit / a.H, h = unit - p * a.H;
   const Tokens tk = tokens_between(a, p, p + 1);
   const int rows = min(tk.count, kSmallRows) * a.G;              // (a count past it is not this kernel's, and no product overflows)
-  if (rows == 0 || tk.count > kSmallRows || rows > MT * 16) return;
+  if (rows == 0 || tk.count > kSmallRows || rows > a.small_rows) return;
   const int len = clampi(a.kv_len[p], 0, a.N);
   const int group = group_of(a, p), base = prefix_of(a, group);
   const int r0 = len - tk.count;                                 // row of the first new token

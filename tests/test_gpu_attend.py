@@ -146,6 +146,34 @@ def test_strided_queries_and_outputs_and_rows_behind_the_batch():
         assert (room[n:] == 9).all() and (room[:, :2] == 9).all() and (room[:, 8:] == 9).all() and (lse[n:] == 4).all()
 
 
+@pytest.mark.parametrize("G, new", [(5, [4, 1, 5, 0, 3]), (8, [2, 2, 4, 1]), (32, [1, 1, 1, 0]), (17, [1, 0])])
+def test_some_rows_over_large_caches(G, new):
+    """17 to 32 rows of queries, problems with fewer among them, in caches that are large or only have the room."""
+    rooms = [900000 // len(new) + 1, 1 << 18]
+    for N in rooms:
+        lens = [(7000, 300, n + 1, 0, 2000)[i % 5] + n for i, n in enumerate(new)]
+        b = Batch(1, G, new, lens, page=0, seed=23)
+        k, v = (torch.empty((len(new), 1, N, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        k[:, :, :b.N], v[:, :, :b.N] = b.rows_k, b.rows_v
+        shape = rkv.Shape(num_problems=len(new), kv_heads=1, q_heads=G, n_tokens=N, budget=N - 1)
+        for window, sinks in ((0, 0), (50, 4)):
+            got = rkv.rkv_attend(shape, b.q, k, v, b.starts, b.kv_len, window=window, sinks=sinks, max_new=max(new), want_lse=True,
+                                 ws=rkv.make_attend_workspace(shape, b.T, max(new)))
+            check(got, attend64(b, window, sinks), f"{N} rows, window {window}")
+
+
+@pytest.mark.parametrize("pad", [0, 3, 500])
+def test_few_rows_among_prompts_with_and_without_padding(pad):
+    """Whether the token array leaves room for a problem with few rows or not, it is attended."""
+    for new, lens in (([40, 40, 40], [40, 300, 41]), ([40, 1, 40], [100, 900, 40]), ([40, 39, 2], [40, 39, 700]), ([9, 9, 8], [20, 9, 500])):
+        b = Batch(2, 4, new, lens, seed=24, extra_tokens=pad, page=16)
+        n = sum(new)
+        out, lse = torch.full_like(b.q, 3.0), torch.full(b.q.shape[:2], 4.0, device="cuda")
+        run(b, out=out, lse=lse)
+        check((out[:n], lse[:n]), tuple(t[:n] for t in attend64(b)), f"{new}")
+        assert (out[n:] == 3).all() and (lse[n:] == 4).all()
+
+
 def test_a_token_array_that_is_mostly_padding():
     """Parts that do not lie by token, joined unit by unit; what is behind the batch stays as it was."""
     b = Batch(2, 4, [1, 2, 1], [3000, 700, 5000], seed=21, page=16, extra_tokens=3000)
