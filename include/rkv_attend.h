@@ -58,7 +58,7 @@ rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_param
 /*
  * rkv_attend: attention of the new tokens over their problems' caches, which hold them already.  With n new tokens and
  * L = kv_len[p] rows, token j is row r = L - n + j and sees the rows c <= r; with window > 0 of those only
- * c > r - window and c < sinks.  out[t, hq] = sum_c w_c v_c, w = softmax over the visible rows of scale * q . k_c;
+ * c > r - window or c < sinks.  out[t, hq] = sum_c w_c v_c, w = softmax over the visible rows of scale * q . k_c;
  * lse[t, hq] (fp32, dense, NULL: not wanted) = log sum_c exp(scale * q . k_c).  A token without a visible row (r < 0) gets zeros and
  * -infinity.  What a token does not see has no influence on it, infinities and NaN included.  Sums and the softmax are held in fp32; the
  * weights are rounded to bf16 before they are multiplied with v.
