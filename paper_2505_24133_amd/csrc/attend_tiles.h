@@ -11,7 +11,7 @@
 // The largest prompts run at 1.03 PFLOP/s (three of up to 15000 tokens, 32 heads on 8: 600 us) where a library product of 8192^3 reaches
 // 1.30 and the same matrix and vector instructions with nothing to wait for 1.6; without the copies it would be 540 us, without
 // the reads of LDS too 489: LDS delivers 128 bytes a cycle, just what 32 query rows a wave use of it, and the clock falls with the power
-// that the products draw.  48 query rows a wave (16x16x32) win 3 % there and lose 7 to 15 where there are edges or few tiles; 64, one
+// that the products draw.  48 query rows a wave (16x16x32) win 3 % there and lose 7 to 18 where there are edges or few tiles; 64, one
 // wave a SIMD, take 1.5 times as long.
 #pragma once
 
