@@ -166,20 +166,22 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   // (where a problem with so few would leave the others more than max_new each there is none, unless tokens are padding: the many-rows
   // kernel has it then)
   const bool small = !large || (c.P > 1 && c.G <= kSmallRows && (int64_t)t.tokens * c.G - (int64_t)(c.P - 1) * most_rows <= kSmallRows);
-  // rows that a query may see, at most
-  const int64_t reach = t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + t.max_new) : c.N;
+  // rows that the queries of a unit or a tile, which have so many tokens, may see
+  auto reach = [&](int64_t tokens) {
+    return t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + std::min<int64_t>(tokens, t.max_new)) : (int64_t)c.N;
+  };
   if (small) {
     a.small_rows = most_rows <= 16 || (heavy && most_rows <= kSmallRows) ? 16 : kSmallRows;
-    split_small((int64_t)c.P * c.H, reach, &a);
+    split_small((int64_t)c.P * c.H, reach(a.small_rows / c.G), &a);
     // (a workgroup a row, which the join takes for more than 32 parts, would be more threads than a launch has)
     if (rows > (1 << 22)) a.small_splits = std::min(a.small_splits, 30);
     // (a token array that is mostly padding would make for large parts by token)
     a.small_by_token = !large && rows <= (int64_t)c.P * c.H * a.small_rows;
   }
-  if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach, c.N);
+  if (large) a.tile_splits = split_tiles(attend_tile_bound(t.tokens, c.G, c.P) * c.H, rows, reach(kTileRows / c.G + 2), c.N);
   if (t.groups > 0) {
     const int64_t tiles = attend_tile_bound(t.tokens, c.G, t.groups) * c.H;
-    a.prefix_splits = !large ? split_prefix(tiles, rows, reach, (int64_t)c.P * c.H, c.N) : split_tiles(tiles, rows, reach, c.N);
+    a.prefix_splits = !large ? split_prefix(tiles, rows, reach(t.max_new), (int64_t)c.P * c.H, c.N) : split_tiles(tiles, rows, reach(t.max_new), c.N);
   }
   if ((int64_t)c.P * c.H * std::max(a.small_splits, 1) > kMaxBlocks ||
       attend_tile_bound(t.tokens, c.G, c.P) * c.H * std::max(std::max(a.tile_splits, a.prefix_splits), 1) > kMaxBlocks ||
