@@ -183,14 +183,18 @@ bool caches_of(PyObject* shape, PyObject* k, PyObject* v, int device, Caches* c)
   return ok;
 }
 
-// bf16 [T, heads, d] with a contiguous last dimension; its strides, 0 where there is one entry only.
+// bf16 [T, heads, d] with a contiguous last dimension, and its strides: 0, 0 says dense, where there is one token or one head only its
+// stride is the dense one, and an array with a broadcast dimension is not taken (its strides of 0 would say dense).
 const at::Tensor* tokens_of(PyObject* o, int64_t T, int64_t heads, int64_t d, int device, int64_t* st, int64_t* sh) {
   const at::Tensor* t = here(o, at::kBFloat16, device);
   if (t == nullptr || t->dim() != 3 || t->size(0) != T || t->size(1) != heads || t->size(2) != d || t->stride(2) != 1) return nullptr;
-  const bool dense = t->is_contiguous();
-  *st = dense || T == 1 ? 0 : t->stride(0);
-  *sh = dense || heads == 1 ? 0 : t->stride(1);
-  return t;
+  if (t->is_contiguous()) {
+    *st = *sh = 0;
+    return t;
+  }
+  *st = T == 1 ? heads * d : t->stride(0);
+  *sh = heads == 1 ? d : t->stride(1);
+  return *st != 0 && *sh != 0 ? t : nullptr;
 }
 bool int_arg(PyObject* o, int64_t* out) {
   int over = 0;

@@ -526,11 +526,16 @@ def _check_list(t: torch.Tensor, entries: int, what: str) -> None:
         raise ValueError(f"{what} must be contiguous int32 [{entries}], got {tuple(t.shape)} {t.dtype}")
 
 
-def _token_strides(t: torch.Tensor) -> Tuple[int, int]:
-    """Token and head strides in elements, 0 where there is one entry only (0, 0: dense)."""
+def _token_strides(t: torch.Tensor, what: str) -> Tuple[int, int]:
+    """Token and head strides in elements; 0, 0 says dense, which an array with a broadcast dimension is not: that is refused.  Where there is
+    one token or one head only, its stride is the dense one."""
     if t.is_contiguous():
         return 0, 0
-    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+    st = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    sh = t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    if st == 0 or sh == 0:
+        raise ValueError(f"{what} has a broadcast dimension (strides {t.stride()}): every token and head needs a row of its own")
+    return st, sh
 
 
 def _pages(shape: Shape, k: torch.Tensor, v: torch.Tensor) -> int:
@@ -572,8 +577,8 @@ def rkv_cache_append_rotary(shape: Shape, k_cache: torch.Tensor, v_cache: torch.
         _check_list(t, entries, what)
     prm = shape.params(k_cache, v_cache, q=q_cache)
     rot = RkvRotaryParams(T, 2 * cos.shape[1], int(bool(interleaved)), cos.shape[0], _pages(shape, k_cache, v_cache), _ptr(cos), _ptr(sin),
-                          _ptr(starts), _ptr(held), _ptr(seen), *_token_strides(k_new), *_token_strides(v_new), *_token_strides(q_new),
-                          *_token_strides(q_out))
+                          _ptr(starts), _ptr(held), _ptr(seen), *_token_strides(k_new, "k_new"), *_token_strides(v_new, "v_new"),
+                          *_token_strides(q_new, "q_new"), *_token_strides(q_out, "q_out"))
     s = load_library().rkv_cache_append_rotary(ctypes.byref(prm), ctypes.byref(rot), _ptr(k_cache), _ptr(v_cache), _ptr(q_cache), _ptr(k_new),
                                                _ptr(v_new), _ptr(q_new), _ptr(q_out), _stream())
     if s != RKV_OK:
@@ -629,7 +634,7 @@ def _attend(shape: Shape, q, k, v, starts, kv_len, group_starts, prefix_len, win
     prm = shape.params(k, v)
     att = RkvAttendParams(T, T if max_new is None else max_new, window, sinks, groups, _pages(shape, k, v),
                           shape.head_dim ** -0.5 if scale is None else scale, _ptr(starts), _ptr(kv_len), _ptr(group_starts), _ptr(prefix_len),
-                          *_token_strides(q), *_token_strides(out))
+                          *_token_strides(q, "q"), *_token_strides(out, "out"))
     lib = load_library()
     if ws is None:
         n = ctypes.c_size_t(0)

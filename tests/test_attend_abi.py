@@ -241,3 +241,51 @@ def test_outputs_whose_rows_lie_in_each_other_are_refused(lib):
         assert got == want or (good and got == rkv.RKV_ERR_UNSUPPORTED), (st, sh, tokens)
         # queries may lie in each other
         assert size(lib, p, att(q_stride_token=max(st, 8), q_stride_head=sh, **one_each))[0] != rkv.RKV_ERR_SHAPE
+
+
+class _NotReached:
+    def __getattr__(self, name):
+        raise AssertionError(f"{name} was reached")
+
+
+def _broadcast(T, heads):
+    """Arrays [T, heads, d] of fewer rows than they have places: strides of 0 in every dimension that has more than one entry, or in one."""
+    one = torch.zeros((1, 1, 128), dtype=torch.bfloat16)
+    made = [one.expand(T, heads, 128)]
+    if T > 1 and heads > 1:
+        made += [torch.zeros((1, heads, 128), dtype=torch.bfloat16).expand(T, -1, -1), torch.zeros((T, 1, 128), dtype=torch.bfloat16).expand(-1, heads, -1)]
+    return made
+
+
+@pytest.mark.parametrize("T,H,G", [(5, 1, 1), (5, 2, 4), (1, 2, 4), (1, 1, 8)])
+def test_broadcast_token_arrays_are_refused(monkeypatch, T, H, G):
+    """Strides of 0 are the library's word for dense: an array whose rows are fewer than its places never gets there, to be read or written
+    as if it had them all."""
+    s = shape(num_problems=1, kv_heads=H, q_heads=H * G, n_tokens=64, budget=32)
+    native = lambda *args: None  # noqa: E731
+    for name, value in (("_need_here", lambda *args: None), ("_append_rotary", native), ("_attend_native", native), ("load_library", _NotReached), ("_stream", lambda: 0)):
+        monkeypatch.setattr(rkv, name, value)
+    kv = torch.zeros((1, H, 64, 128), dtype=torch.bfloat16)
+    one, two = torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    table = torch.zeros((10, 64))
+    good = {"k_new": torch.zeros((T, H, 128)).bfloat16(), "v_new": torch.zeros((T, H, 128)).bfloat16(), "q_new": torch.zeros((T, H * G, 128)).bfloat16(),
+            "q_out": torch.zeros((T, H * G, 128)).bfloat16()}
+    for name, heads in (("k_new", H), ("v_new", H), ("q_new", H * G), ("q_out", H * G)):
+        if T == heads == 1:
+            continue
+        for bad in _broadcast(T, heads):
+            a = {**good, name: bad}
+            with pytest.raises(ValueError, match=f"{name} has a broadcast dimension"):
+                rkv.rkv_cache_append_rotary(s, kv, kv, None, a["k_new"], a["v_new"], a["q_new"], table, table, two, one, one, q_out=a["q_out"])
+    for bad in _broadcast(T, H * G):
+        with pytest.raises(ValueError, match="q has a broadcast dimension"):
+            rkv.rkv_attend(s, bad, kv, kv, two, one, ws=torch.zeros(0, dtype=torch.uint8))
+        with pytest.raises(ValueError, match="out has a broadcast dimension"):
+            rkv.rkv_attend_shared(s, good["q_new"], kv, kv, two, one, one, one[:0], out=bad, ws=torch.zeros(0, dtype=torch.uint8))
+
+
+def test_strides_of_one_token_or_one_head_are_the_dense_ones():
+    room = torch.zeros((5, 6, 256), dtype=torch.bfloat16)
+    for t, want in ((room[..., :128], (1536, 256)), (room[:1, :, :128], (6 * 128, 256)), (room[:, :1, :128], (1536, 128)), (room[:1, :1, :128], (0, 0)),
+                    (torch.zeros((5, 6, 128)), (0, 0)), (room[:0, :, :128], (0, 0))):
+        assert rkv._token_strides(t, "q") == want

@@ -123,3 +123,41 @@ def test_what_the_binding_refuses(path):
     with pytest.raises(ValueError, match="group_starts must be"):
         rkv.rkv_attend_shared(*lists, int32([0, 1]), int32([1, 2]))
     check(rkv.rkv_attend(*lists, want_lse=True), attend64(b))
+
+
+@pytest.mark.parametrize("T,H,G", [(5, 1, 1), (5, 2, 3), (1, 2, 3), (1, 1, 6)])
+def test_broadcast_token_arrays_are_refused(path, T, H, G):
+    """Arrays whose rows are fewer than their places: refused on the host by both paths, whichever array it is."""
+    b = Batch(H, G, [T], [40], seed=6)
+    one = torch.zeros((1, 1, 128), dtype=torch.bfloat16, device="cuda")
+    cos, sin = rkv.rotary_tables(50)
+    new = {"k_new": one.repeat(T, H, 1), "v_new": one.repeat(T, H, 1), "q_new": one.repeat(T, H * G, 1), "q_out": one.repeat(T, H * G, 1)}
+    before = b.k.clone(), b.v.clone()
+    for name, t in new.items():
+        if t.shape[0] == t.shape[1] == 1:
+            continue
+        bad = {**new, name: one.expand(t.shape)}
+        with pytest.raises(ValueError, match="broadcast dimension"):
+            rkv.rkv_cache_append_rotary(b.shape, b.k, b.v, None, bad["k_new"], bad["v_new"], bad["q_new"], cos, sin, b.starts, int32([3]), int32([3]), q_out=bad["q_out"])
+    assert torch.equal(b.k, before[0]) and torch.equal(b.v, before[1])
+    if T * H * G > 1:
+        room = rkv.make_attend_workspace(b.shape, T)
+        for kw in (dict(), dict(ws=room)):
+            with pytest.raises(ValueError, match="broadcast dimension"):
+                rkv.rkv_attend(b.shape, one.expand(b.q.shape), b.k, b.v, b.starts, b.kv_len, **kw)
+            with pytest.raises(ValueError, match="broadcast dimension"):
+                rkv.rkv_attend(b.shape, b.q, b.k, b.v, b.starts, b.kv_len, out=one.expand(b.q.shape), **kw)
+
+
+def test_one_token_or_one_head_in_wider_rows(path):
+    """Token arrays with one token or one head, not dense: read and written where they lie."""
+    for new, H, G in (([1], 2, 3), ([6], 1, 1)):
+        b = Batch(H, G, new, [300], seed=7)
+        wide = torch.full((b.T, H * G, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+        wide[..., :128] = b.q
+        room = torch.full_like(wide, 9.0)
+        lse = torch.empty(b.q.shape[:2], device="cuda")
+        out, _ = rkv.rkv_attend(b.shape, wide[..., :128], b.k, b.v, b.starts, b.kv_len, max_new=new[0], out=room[..., :128], lse=lse,
+                                ws=rkv.make_attend_workspace(b.shape, b.T, new[0]))
+        check((out, lse), attend64(b))
+        assert (room[..., 128:] == 9).all()
