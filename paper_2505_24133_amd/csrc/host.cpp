@@ -56,12 +56,15 @@ bool float_field(PyObject* shape, Field f, float* out) {
   return is_float;
 }
 
+// Strides of 0 in all dimensions but the last say dense to the library, which one row broadcast to all places is not.
+bool rows_apart(const at::Tensor& t) { return t.stride(0) != 0 || t.stride(1) != 0 || t.stride(2) != 0 || t.is_contiguous(); }
+
 // A plain strided bf16 tensor in GPU memory with the given sizes; `dense`: contiguous, else only its last dimension.
 const at::Tensor* plain(PyObject* o, at::IntArrayRef sizes, bool dense) {
   if (!THPVariable_CheckExact(o)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || t.scalar_type() != at::kBFloat16 ||
-      t.sizes() != sizes || (dense ? !t.is_contiguous() : t.stride(3) != 1))
+      t.sizes() != sizes || (dense ? !t.is_contiguous() : t.stride(3) != 1 || !rows_apart(t)))
     return nullptr;
   return &t;
 }
@@ -160,7 +163,7 @@ bool caches_of(PyObject* shape, PyObject* k, PyObject* v, int device, Caches* c)
   if (c->k == nullptr || c->v == nullptr || c->k->dim() != 4 || c->v->dim() != 4 || c->k->stride(3) != 1 || c->v->stride(3) != 1) return false;
   const int64_t rows = page > 0 ? page : c->N;
   for (const at::Tensor* t : {c->k, c->v})
-    if ((page == 0 && t->size(0) != c->P) || t->size(1) != c->H || t->size(2) != rows || t->size(3) != c->d) return false;
+    if ((page == 0 && t->size(0) != c->P) || t->size(1) != c->H || t->size(2) != rows || t->size(3) != c->d || !rows_apart(*t)) return false;
   rkv_params& p = c->p;
   p.num_problems = (int32_t)c->P; p.kv_heads = (int32_t)c->H; p.q_heads = (int32_t)c->Hq; p.n_tokens = (int32_t)c->N; p.head_dim = (int32_t)c->d;
   p.alpha = (int32_t)c->alpha;
@@ -230,7 +233,7 @@ PyObject* append_rotary(PyObject*, PyObject* const* args, Py_ssize_t count) {
     void* ring = nullptr;
     if (args[3] != Py_None) {
       const at::Tensor* t = here(args[3], at::kBFloat16, device);
-      if (t == nullptr || t->sizes() != at::IntArrayRef({c.P, c.Hq, c.alpha, c.d}) || t->stride(3) != 1) Py_RETURN_NONE;
+      if (t == nullptr || t->sizes() != at::IntArrayRef({c.P, c.Hq, c.alpha, c.d}) || t->stride(3) != 1 || !rows_apart(*t)) Py_RETURN_NONE;
       if (!t->is_contiguous()) { c.p.q_stride_problem = t->stride(0); c.p.q_stride_head = t->stride(1); c.p.q_stride_token = t->stride(2); }
       ring = t->data_ptr();
     }

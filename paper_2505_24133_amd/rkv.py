@@ -141,6 +141,14 @@ def status_string(status: int) -> str:
     return load_library().rkv_status_string(int(status)).decode()
 
 
+def _row_strides(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
+    """Strides of [problems, heads, rows, d] without the last.  0, 0, 0 says dense, which one row broadcast to all places is not."""
+    s = t.stride()[:3]
+    if s == (0, 0, 0) and not t.is_contiguous():
+        raise ValueError(f"{what} is one row broadcast to all places {tuple(t.shape)}: every row needs its own")
+    return s
+
+
 @dataclass
 class Shape:
     num_problems: int
@@ -163,8 +171,8 @@ class Shape:
 
     def params(self, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None) -> RkvParams:
-        ks = (0, 0, 0) if k is None or self.page_size else k.stride()[:3]
-        vs = (0, 0, 0) if v is None or self.page_size else v.stride()[:3]
+        ks = (0, 0, 0) if k is None or self.page_size else _row_strides(k, "k")
+        vs = (0, 0, 0) if v is None or self.page_size else _row_strides(v, "v")
         p = RkvParams()
         try:
             # one call for all fields: a third of the time of setting them one by one
@@ -177,7 +185,7 @@ class Shape:
                           self.budget, self.pool_w, self.beta, self.sim_threshold, self.lam, self.eps, self.flags,
                           *ks, *vs)
         if q is not None and not q.is_contiguous():
-            p.q_stride_problem, p.q_stride_head, p.q_stride_token = q.stride(0), q.stride(1), q.stride(2)
+            p.q_stride_problem, p.q_stride_head, p.q_stride_token = _row_strides(q, "q")
         if self.page_size:
             bt = self.block_table
             if bt is None or bt.dtype != torch.int32 or not bt.is_cuda or not bt.is_contiguous() or bt.dim() != 2 \
@@ -192,10 +200,10 @@ class Shape:
                 setattr(p, f"{name}_stride_head", sh)
                 setattr(p, f"{name}_stride_token", st)
             if out is not None and not out.is_contiguous():
-                p.o_stride_problem, p.o_stride_head, p.o_stride_token = out.stride(0), out.stride(1), out.stride(2)
+                p.o_stride_problem, p.o_stride_head, p.o_stride_token = _row_strides(out, "out")
             return p
         if out is not None and not out.is_contiguous():
-            p.o_stride_problem, p.o_stride_head, p.o_stride_token = out.stride(0), out.stride(1), out.stride(2)
+            p.o_stride_problem, p.o_stride_head, p.o_stride_token = _row_strides(out, "out")
         return p
 
     @property

@@ -289,3 +289,39 @@ def test_strides_of_one_token_or_one_head_are_the_dense_ones():
     for t, want in ((room[..., :128], (1536, 256)), (room[:1, :, :128], (6 * 128, 256)), (room[:, :1, :128], (1536, 128)), (room[:1, :1, :128], (0, 0)),
                     (torch.zeros((5, 6, 128)), (0, 0)), (room[:0, :, :128], (0, 0))):
         assert rkv._token_strides(t, "q") == want
+
+
+@pytest.mark.parametrize("which", ["k", "v", "q", "out"])
+@pytest.mark.parametrize("entry", ["params", "append", "append_rotary", "attend", "compress"])
+def test_one_row_as_a_whole_cache_is_refused(monkeypatch, which, entry):
+    """Strides of 0, 0, 0 are the library's word for dense: one row broadcast to a cache's places never gets there."""
+    s = shape(num_problems=2, kv_heads=2, q_heads=4, n_tokens=64, budget=32)
+    native = lambda *args: None  # noqa: E731
+    for name, value in (("_need_here", lambda *args: None), ("_need_gpu", lambda *args: None), ("_append", native), ("_append_rotary", native),
+                        ("_attend_native", native), ("load_library", _NotReached), ("_stream", lambda: 0), ("_ws_args", lambda *args: (None, 0, 0))):
+        monkeypatch.setattr(rkv, name, value)
+    a = {"k": torch.zeros((2, 2, 64, 128)), "v": torch.zeros((2, 2, 64, 128)), "q": torch.zeros((2, 4, 8, 128)), "out": torch.zeros((2, 2, 32, 128))}
+    a = {name: t.bfloat16() for name, t in a.items()}
+    a[which] = torch.zeros((1, 1, 1, 128), dtype=torch.bfloat16).expand(a[which].shape)
+    new = {h: torch.zeros((2, h, 128), dtype=torch.bfloat16) for h in (2, 4)}
+    two, three = torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    table = torch.zeros((10, 64))
+    if (which, entry) in (("out", "append"), ("out", "append_rotary"), ("q", "attend"), ("out", "attend")):
+        pytest.skip("not an argument of this call")
+    with pytest.raises(ValueError, match=f"{which} is one row broadcast"):
+        if entry == "params":
+            s.params(a["k"], a["v"], a["out"], a["q"])
+        elif entry == "append":
+            rkv.rkv_cache_append(s, a["k"], a["v"], a["q"], new[2], new[2], new[4], 0, 0)
+        elif entry == "append_rotary":
+            rkv.rkv_cache_append_rotary(s, a["k"], a["v"], a["q"], new[2], new[2], new[4], table, table, three, two, two)
+        elif entry == "attend":
+            rkv.rkv_attend(s, new[4], a["k"], a["v"], three, two, ws=torch.zeros(0, dtype=torch.uint8))
+        else:
+            rkv.rkv_compress(s, a["q"], a["k"], a["v"], k_out=a["out"], v_out=a["out"])
+
+
+def test_one_row_is_dense_where_there_is_one_place():
+    one = torch.zeros(128, dtype=torch.bfloat16).as_strided((1, 1, 1, 128), (0, 0, 0, 1))
+    assert rkv._row_strides(one, "k") == (0, 0, 0)
+    assert rkv._row_strides(torch.zeros((2, 3, 5, 256))[..., :128], "k") == (3840, 1280, 256)

@@ -161,3 +161,20 @@ def test_one_token_or_one_head_in_wider_rows(path):
                                 ws=rkv.make_attend_workspace(b.shape, b.T, new[0]))
         check((out, lse), attend64(b))
         assert (room[..., 128:] == 9).all()
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_one_row_as_a_whole_cache_is_refused(path, which):
+    """A cache (of keys, values, queries) that is one row broadcast to all places: refused on the host by both paths, in every call that takes one."""
+    b = Batch(2, 3, [1, 1], [40, 30], seed=8)
+    caches = [b.k, b.v, torch.zeros((2, 6, b.shape.alpha, 128), dtype=torch.bfloat16, device="cuda")]
+    caches[which] = torch.zeros(128, dtype=torch.bfloat16, device="cuda").expand(caches[which].shape)
+    cos, sin = rkv.rotary_tables(50)
+    kv = torch.ones((2, 2, 128), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="one row broadcast"):
+        rkv.rkv_cache_append(b.shape, *caches, kv, kv, b.q, 3, 3)
+    with pytest.raises(ValueError, match="one row broadcast"):
+        rkv.rkv_cache_append_rotary(b.shape, *caches, kv, kv, b.q, cos, sin, b.starts, int32([3, 3]), int32([3, 3]))
+    if which < 2:
+        with pytest.raises(ValueError, match="one row broadcast"):
+            rkv.rkv_attend(b.shape, b.q, caches[0], caches[1], b.starts, b.kv_len, ws=rkv.make_attend_workspace(b.shape, b.T))
