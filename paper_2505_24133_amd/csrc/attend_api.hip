@@ -146,7 +146,8 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
     return RKV_ERR_SHAPE;
   a.starts = t.starts; a.kv_len = t.kv_len; a.group_starts = t.group_starts; a.prefix_len = t.prefix_len;
   a.P = c.P; a.H = c.H; a.G = c.G; a.N = c.N; a.T = t.tokens; a.groups = t.groups;
-  a.window = t.window; a.sinks = t.sinks; a.num_pages = t.num_pages;
+  // (a window of N rows hides nothing, and a larger one would take the lowest row that a token before the first one sees past 32 bits)
+  a.window = std::min(t.window, c.N); a.sinks = t.sinks; a.num_pages = t.num_pages;
   a.kl = c.kl; a.vl = c.vl;
   a.scale2 = t.scale * 1.4426950408889634f;
   pl->paged = c.paged;

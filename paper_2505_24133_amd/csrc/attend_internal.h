@@ -78,7 +78,8 @@ __device__ __forceinline__ int group_of(const AttendArgs& a, int p) {
 }
 __device__ __forceinline__ int prefix_of(const AttendArgs& a, int g) { return g < 0 ? 0 : clampi(a.prefix_len[g], 0, a.N); }
 
-// What the token at row r of its problem may see: rows c < hi with c >= lo or c < sinks.
+// What the token at row r of its problem may see: rows c < hi with c >= lo or c < sinks.  r is -2^24 at least (a token before the first
+// row), and the window n_tokens at most, 2^24, so that nothing here passes 32 bits.
 struct Sight { int lo, hi; };
 __device__ __forceinline__ Sight sight(const AttendArgs& a, int r) {
   return Sight{a.window > 0 ? max(r - a.window + 1, 0) : 0, max(r + 1, 0)};

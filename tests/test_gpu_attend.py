@@ -291,3 +291,13 @@ def test_cache_past_32_bits_of_offset():
         values[table[p].long()] = b.rows_v[p].reshape(1, N // 16, 16, 128).transpose(0, 1)
     shape.page_size, shape.block_table = 16, table
     check(rkv.rkv_attend(shape, b.q, pool, values, b.starts, b.kv_len, max_new=1, want_lse=True), attend64(b))
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 24 + 1, 201, 200, 3])
+@pytest.mark.parametrize("sinks", [0, 2, 2 ** 31 - 1])
+def test_rows_that_see_nothing_under_any_window(window, sinks):
+    """Fewer rows than new tokens and a window of any size: the first tokens see nothing, the others of the same problem what they see."""
+    print(f"[gpu-case] attend, tokens before the first row, window={window} sinks={sinks}", flush=True)
+    for page in (0, 16):
+        for new, lens in (([5, 8, 2, 8], [2, 1, 0, 200]), ([90, 40, 33], [33, 2, 0]), ([200, 3, 1], [150, 1, 120]), ([130], [7])):
+            both(Batch(2, 4, new, lens, N=200, page=page, seed=25), window, sinks, where=f"{new} {lens} page {page}")

@@ -140,3 +140,15 @@ def test_graph_and_workspace():
         check((out, lse), attend64(b))
         eager = run(b)
         assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 24 + 1, 400, 30])
+@pytest.mark.parametrize("G,new", [(4, [5]), (4, [40]), (40, [3, 9])])
+def test_tokens_before_the_first_row_under_any_window(window, G, new):
+    """Fewer rows than new tokens, in a group too: the first ones see nothing, the others what they see."""
+    print(f"[gpu-case] attend shared, tokens before the first row, window={window} G={G} new={new}", flush=True)
+    b = grouped(2, G, [4], [100], new, [50], outside=1, seed=12)
+    b.lens = [150 + new[0], 60, 2, 1, 3]
+    b.kv_len.copy_(int32(b.lens))
+    for sinks in (0, 2):
+        check(run(b, window, sinks), attend64(b, window, sinks), f"sinks {sinks}")
