@@ -100,6 +100,10 @@ class DecodeCache:
             self._attend_room[n] = rkv.rkv_attend_workspace_size(s, P * n, n, 0 if self._groups is None else self._groups[1].shape[0])
         if self._attend_ws is None or self._attend_ws.numel() < self._attend_room[n] + 256:
             self._attend_ws = torch.empty(self._attend_room[n] + 256, dtype=torch.uint8, device=self.q_cache.device)
+        # what attention may refuse is refused here, and its output made: behind the append the query cache has lost the slots that the new
+        # queries take, so nothing may fail there
+        rkv._check_sight(window, sinks, n, scale, "DecodeCache.step")
+        out = torch.empty((P * n, s.q_heads, s.head_dim), dtype=torch.bfloat16, device=self.q_cache.device)
         starts, k, v = self._starts[n], self.k, self.v
         # positions count from the last multiple of alpha, whose rows of the tables come first: the slots of the query cache go by them
         slot = self.tokens_seen % s.alpha
@@ -107,11 +111,11 @@ class DecodeCache:
         q = rkv.rkv_cache_append_rotary(s, k, v, self.q_cache, k_new.flatten(0, 1), v_new.flatten(0, 1), q_new.flatten(0, 1), cos[at:], sin[at:],
                                         starts, self._counts[self.length], self._counts[slot], interleaved=interleaved)
         lens = self._counts[self.length + n]
-        common = dict(window=window, sinks=sinks, scale=scale, max_new=n, ws=self._attend_ws)
+        common = dict(window=window, sinks=sinks, scale=scale, max_new=n, ws=self._attend_ws, out=out)
         if self._groups is None:
-            out = rkv.rkv_attend(s, q, k, v, starts, lens, **common)
+            rkv.rkv_attend(s, q, k, v, starts, lens, **common)
         else:
-            out = rkv.rkv_attend_shared(s, q, k, v, starts, lens, *self._groups, **common)
+            rkv.rkv_attend_shared(s, q, k, v, starts, lens, *self._groups, **common)
         self.length += n                                   # (a step that was refused has not taken place)
         self.tokens_seen += n
         if self.length >= s.n_tokens > s.budget:

@@ -7,6 +7,8 @@ library is missing or no GPU is present the calls raise.
 from __future__ import annotations
 
 import ctypes
+import math
+import operator
 import os
 import struct
 from dataclasses import dataclass, field
@@ -610,6 +612,16 @@ def make_attend_workspace(shape: Shape, tokens: int, max_new: Optional[int] = No
     return torch.empty(rkv_attend_workspace_size(shape, tokens, max_new, groups) + 256, dtype=torch.uint8, device=device)
 
 
+def _check_sight(window, sinks, max_new, scale, where: str) -> None:
+    """What attention refuses of these, with the errors that it refuses them with."""
+    if not all(0 <= n <= _INT32_MAX for n in (window, sinks, max_new)):
+        raise ValueError("window, sinks and max_new must be in 0 .. 2^31 - 1")
+    for n in (window, sinks, max_new):
+        operator.index(n)
+    if scale is not None and not 0.0 < ctypes.c_float(scale).value < math.inf:
+        raise RkvError(RKV_ERR_PARAM, where)
+
+
 def _attend(shape: Shape, q, k, v, starts, kv_len, group_starts, prefix_len, window, sinks, scale, max_new, ws, out, lse, want_lse, where):
     if _attend_native is None:
         load_library()
@@ -626,8 +638,7 @@ def _attend(shape: Shape, q, k, v, starts, kv_len, group_starts, prefix_len, win
     _check_kv(shape, k, "k")
     _check_kv(shape, v, "v")
     T = q.shape[0]
-    if not all(0 <= n <= _INT32_MAX for n in (window, sinks, 0 if max_new is None else max_new)):
-        raise ValueError("window, sinks and max_new must be in 0 .. 2^31 - 1")
+    _check_sight(window, sinks, 0 if max_new is None else max_new, scale, where)
     _check_tokens(q, (T, shape.q_heads, shape.head_dim), "q")
     _check_tokens(out, (T, shape.q_heads, shape.head_dim), "out")
     if lse is not None and (tuple(lse.shape) != (T, shape.q_heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):

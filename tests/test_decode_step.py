@@ -1,0 +1,81 @@
+"""DecodeCache.step's order of work, with the library's calls replaced by ones that say when they were reached.  CPU only."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_24133_amd import decode, rkv
+
+
+@pytest.fixture
+def reached(monkeypatch):
+    """The calls made, in order; none of them computes anything."""
+    calls = []
+
+    def append(shape, k, v, ring, k_new, v_new, q_new, *args, **kw):
+        calls.append("append")
+        return q_new.clone()
+
+    def attend(shape, q, *args, **kw):
+        calls.append("attend")
+        return kw["out"] if kw.get("out") is not None else torch.empty_like(q)
+
+    def compress(shape, *args, **kw):
+        calls.append("compress")
+        return (rkv.RKV_OK,) * 5
+
+    for name, call in (("rkv_cache_append_rotary", append), ("rkv_attend", attend), ("rkv_attend_shared", attend), ("rkv_compress", compress),
+                       ("rkv_compress_inplace", compress)):
+        monkeypatch.setattr(rkv, name, call)
+    return calls
+
+
+def make(P=2, H=1, G=2, N=40, budget=30, **kw):
+    return decode.DecodeCache(rkv.Shape(num_problems=P, kv_heads=H, q_heads=H * G, n_tokens=N, budget=budget), device="cpu", **kw)
+
+
+def tokens(n, P=2, H=1, G=2):
+    return [torch.zeros((P, n, h, 128), dtype=torch.bfloat16) for h in (H * G, H, H)]
+
+
+TABLES = rkv.rotary_tables(100, device="cpu")
+
+
+@pytest.mark.parametrize("error,kw", [
+    (ValueError, dict(window=-1)), (ValueError, dict(window=2 ** 31)), (ValueError, dict(sinks=-1)), (ValueError, dict(sinks=2 ** 31)),
+    (TypeError, dict(window=1.5)), (TypeError, dict(sinks="2")), (rkv.RkvError, dict(scale=0.0)), (rkv.RkvError, dict(scale=-0.1)),
+    (rkv.RkvError, dict(scale=float("nan"))), (rkv.RkvError, dict(scale=float("inf"))), (rkv.RkvError, dict(scale=1e-60)),
+    (rkv.RkvError, dict(scale=1e60)), (TypeError, dict(scale="1"))])
+@pytest.mark.parametrize("share", [False, True])
+def test_what_attention_refuses_is_refused_before_the_append(reached, error, kw, share):
+    cache = make()
+    if share:
+        cache.step(*tokens(4), *TABLES)
+        cache.share_prompt([2], [4])
+        reached.clear()
+    before = cache.length, cache.tokens_seen
+    with pytest.raises(error):
+        cache.step(*tokens(3), *TABLES, **kw)
+    assert reached == [] and (cache.length, cache.tokens_seen) == before
+    cache.step(*tokens(3), *TABLES, window=np.int64(5), sinks=2 ** 31 - 1, scale=1)
+    assert reached == ["append", "attend"] and cache.length == before[0] + 3
+
+
+def test_an_output_that_cannot_be_made_is_asked_for_before_the_append(reached, monkeypatch):
+    """After the append nothing is allocated: out of memory leaves the caches as they were."""
+    cache = make()
+    cache.step(*tokens(3), *TABLES)
+    reached.clear()
+
+    def none_left(*args, **kw):
+        raise torch.OutOfMemoryError("none left")
+
+    for name in ("empty", "empty_like"):
+        monkeypatch.setattr(torch, name, none_left)
+    with pytest.raises(torch.OutOfMemoryError):
+        cache.step(*tokens(3), *TABLES)
+    assert reached == []
+
+
+def test_a_step_gives_what_attention_wrote(reached):
+    out = make().step(*tokens(3), *TABLES)
+    assert out.shape == (2, 3, 2, 128) and reached == ["append", "attend"]

@@ -108,3 +108,30 @@ def test_one_workspace_for_all_lengths():
         t = [torch.zeros((1, n, h, 128), dtype=torch.bfloat16, device="cuda") for h in (4, 1, 1)]
         cache.step(*t, cos, sin)
         assert cache._attend_ws.numel() <= at_most
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+def test_a_refused_step_leaves_the_query_cache(inplace):
+    """The tokens of a refused step are never seen again: the next step is another one, shorter, and a compression takes the queries of
+    the tokens that were accepted."""
+    print(f"[gpu-case] refused step inplace={inplace}", flush=True)
+    s = shape(2, 1, 2, 40, 30)
+    cos, sin = rkv.rotary_tables(200)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+
+    def tokens(n):
+        return tuple(torch.randn((2, n, h, 128), generator=gen, device="cuda").bfloat16() for h in (2, 1, 1))
+
+    taken, refused = [tokens(n) for n in (33, 1, 3, 2, 1)], tokens(5)
+    straight, stumbling = decode.DecodeCache(s, inplace=inplace), decode.DecodeCache(s, inplace=inplace)
+    for t in taken:
+        for error, kw in ((ValueError, dict(window=-1)), (ValueError, dict(sinks=2 ** 31)), (rkv.RkvError, dict(scale=0.0)), (TypeError, dict(window=1.5))):
+            before = stumbling.q_cache.clone(), stumbling.k.clone(), stumbling.v.clone(), stumbling.length, stumbling.tokens_seen
+            n = min(5, s.n_tokens - stumbling.length)
+            with pytest.raises(error):
+                stumbling.step(*(x[:, :n] for x in refused), cos, sin, **kw)
+            assert torch.equal(stumbling.q_cache, before[0]) and torch.equal(stumbling.k, before[1]) and torch.equal(stumbling.v, before[2])
+            assert (stumbling.length, stumbling.tokens_seen) == before[3:]
+        assert torch.equal(stumbling.step(*t, cos, sin), straight.step(*t, cos, sin))
+    assert straight.compressions == stumbling.compressions == 1 and torch.equal(stumbling.kept_idx, straight.kept_idx)
+    assert torch.equal(stumbling.q_cache, straight.q_cache) and torch.equal(stumbling.k[:, :, :30], straight.k[:, :, :30])
