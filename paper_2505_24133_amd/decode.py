@@ -39,6 +39,7 @@ class DecodeCache:
         self._attend_room = {}     # and how much workspace their attention needs; one workspace serves them all
         self._attend_ws = None
         self._groups = None
+        self._streams = {}         # by handle: the streams that steps were made on
 
     @property
     def k(self) -> torch.Tensor:
@@ -48,6 +49,13 @@ class DecodeCache:
     @property
     def v(self) -> torch.Tensor:
         return self._v[self._cur]
+
+    def _let_go(self, *tensors) -> None:
+        """Tensors that steps have used and that are about to be replaced.  Steps may have been made on other streams than the one they were
+        allocated on: their memory is not given out again before what those streams have been given by now is done."""
+        for t in tensors:
+            for stream in self._streams.values():
+                t.record_stream(stream)
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, q_new: torch.Tensor) -> bool:
         """One decode step: k_new, v_new [P, H, d], q_new [P, Hq, d].  Returns True if the step
@@ -76,6 +84,7 @@ class DecodeCache:
         for n in sizes:
             first.append(first[-1] + n)
         device = self.q_cache.device
+        self._let_go(*self._groups or ())
         self._groups = (torch.tensor(first, dtype=torch.int32, device=device), torch.tensor(rows, dtype=torch.int32, device=device)) if sizes else None
         self._attend_room = {}
 
@@ -99,11 +108,15 @@ class DecodeCache:
         if n not in self._attend_room:
             self._attend_room[n] = rkv.rkv_attend_workspace_size(s, P * n, n, 0 if self._groups is None else self._groups[1].shape[0])
         if self._attend_ws is None or self._attend_ws.numel() < self._attend_room[n] + 256:
+            if self._attend_ws is not None:
+                self._let_go(self._attend_ws)
             self._attend_ws = torch.empty(self._attend_room[n] + 256, dtype=torch.uint8, device=self.q_cache.device)
         # what attention may refuse is refused here, and its output made: behind the append the query cache has lost the slots that the new
         # queries take, so nothing may fail there
         rkv._check_sight(window, sinks, n, scale, "DecodeCache.step")
         out = torch.empty((P * n, s.q_heads, s.head_dim), dtype=torch.bfloat16, device=self.q_cache.device)
+        if self.q_cache.is_cuda and rkv._stream() not in self._streams:
+            self._streams[rkv._stream()] = torch.cuda.current_stream()
         starts, k, v = self._starts[n], self.k, self.v
         # positions count from the last multiple of alpha, whose rows of the tables come first: the slots of the query cache go by them
         slot = self.tokens_seen % s.alpha
@@ -127,6 +140,7 @@ class DecodeCache:
         if self.length != s.n_tokens:
             raise RuntimeError("compress() runs when the cache holds budget + buffer rows")
         if self._groups is not None:
+            self._let_go(*self._groups)
             self._groups, self._attend_room = None, {}
         if self.inplace:
             st, *_ = rkv.rkv_compress_inplace(s, self.q_cache, self.k, self.v, ws=self._ws, kept_idx=self.kept_idx)

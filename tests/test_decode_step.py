@@ -79,3 +79,38 @@ def test_an_output_that_cannot_be_made_is_asked_for_before_the_append(reached, m
 def test_a_step_gives_what_attention_wrote(reached):
     out = make().step(*tokens(3), *TABLES)
     assert out.shape == (2, 3, 2, 128) and reached == ["append", "attend"]
+
+
+def test_what_is_replaced_is_held_for_the_streams_that_use_it(reached, monkeypatch):
+    """A larger workspace, another set of groups, a compression that ends one: what was used until then is let go for every stream of a step."""
+    let_go = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: let_go.append((t.data_ptr(), stream)))
+    cache = make()
+    cache._streams = {0: "one", 7: "other"}
+
+    def replaced(*tensors):
+        assert let_go == [(p, s) for p in tensors for s in ("one", "other")]
+        let_go.clear()
+
+    room = {1: 1000, 3: 5000, 2: 2000, 30: 9000}
+    monkeypatch.setattr(rkv, "rkv_attend_workspace_size", lambda shape, tokens, max_new, groups: room[max_new])
+    cache.step(*tokens(1), *TABLES)
+    replaced()
+    first = cache._attend_ws.data_ptr()
+    cache.step(*tokens(3), *TABLES)
+    replaced(first)
+    cache.step(*tokens(2), *TABLES)
+    replaced()                                             # (the larger one does)
+    cache.share_prompt([2], [4])
+    replaced()
+    lists = [t.data_ptr() for t in cache._groups]
+    cache.share_prompt([1, 1], [4, 3])
+    replaced(*lists)
+    lists, first = [t.data_ptr() for t in cache._groups], cache._attend_ws.data_ptr()
+    cache.step(*tokens(30), *TABLES)
+    replaced(first)
+    cache.step(*tokens(3), *TABLES)
+    assert reached.count("compress") == 0
+    cache.step(*tokens(1), *TABLES)
+    assert reached.count("compress") == 1
+    replaced(*lists)

@@ -135,3 +135,35 @@ def test_a_refused_step_leaves_the_query_cache(inplace):
         assert torch.equal(stumbling.step(*t, cos, sin), straight.step(*t, cos, sin))
     assert straight.compressions == stumbling.compressions == 1 and torch.equal(stumbling.kept_idx, straight.kept_idx)
     assert torch.equal(stumbling.q_cache, straight.q_cache) and torch.equal(stumbling.k[:, :, :30], straight.k[:, :, :30])
+
+
+def test_a_replaced_workspace_is_not_given_out_under_a_step():
+    """A step on another stream than the one that the workspace was allocated on, then a longer one: the smaller workspace, and a replaced
+    list of groups, stay as they are as long as the other stream has work that reads them."""
+    print("[gpu-case] replaced workspace", flush=True)
+    s = shape(1, 1, 4, 4000, 3000)
+    cache = decode.DecodeCache(s)
+    cos, sin = rkv.rotary_tables(4000)
+    t = {n: [torch.zeros((1, n, h, 128), dtype=torch.bfloat16, device="cuda") for h in (4, 1, 1)] for n in (1, 60)}
+    assert rkv.rkv_attend_workspace_size(s, 60, 60, 1) > rkv.rkv_attend_workspace_size(s, 1, 1, 1)
+    cache.step(*t[1], cos, sin)
+    cache.share_prompt([1], [1])
+    cache.step(*t[1], cos, sin)
+    held = [x for x in (cache._attend_ws, *cache._groups)]
+    ptrs, sizes = [x.data_ptr() for x in held], [x.numel() * x.element_size() for x in held]
+    del held
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(200_000_000)                     # (some 100 ms, which end by themselves)
+        cache.step(*t[1], cos, sin)
+        done = torch.cuda.Event()
+        done.record()
+    # a new list and a larger workspace, with the step on the other stream still to come
+    cache.share_prompt([1], [2])
+    with torch.cuda.stream(other):
+        cache.step(*t[60], cos, sin)
+    given = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(20)]
+    assert not done.query()
+    assert not {x.data_ptr() for x in given} & set(ptrs)
+    torch.cuda.synchronize()
