@@ -164,15 +164,16 @@ rkv_status plan_attend(const rkv_params* prm, const rkv_attend_params* att, bool
   // behind 1000 rows of 64 sequences 46 and 47, behind prefixes 33 and 46.
   const bool heavy = most_rows > 16 && t.groups == 0 && (int64_t)c.P * c.H * c.N >= 900000;
   const bool large = most_rows > kSmallRows || heavy;
-  // (where a problem with so few would leave the others more than max_new each there is none, unless tokens are padding: the many-rows
-  // kernel has it then)
-  const bool small = !large || (c.P > 1 && c.G <= kSmallRows && (int64_t)t.tokens * c.G - (int64_t)(c.P - 1) * most_rows <= kSmallRows);
+  // Rows of queries that the few-rows kernel takes of a problem, if it runs; and whether a problem may have so few (where one would leave the
+  // others more than max_new each there is none, unless tokens are padding: the many-rows kernel has it then).
+  const int small_rows = most_rows <= 16 || (heavy && most_rows <= kSmallRows) ? 16 : kSmallRows;
+  const bool small = !large || (c.P > 1 && c.G <= small_rows && (int64_t)t.tokens * c.G - (int64_t)(c.P - 1) * most_rows <= small_rows);
   // rows that the queries of a unit or a tile, which have so many tokens, may see
   auto reach = [&](int64_t tokens) {
     return t.window > 0 ? std::min<int64_t>(c.N, (int64_t)t.window + t.sinks + std::min<int64_t>(tokens, t.max_new)) : (int64_t)c.N;
   };
   if (small) {
-    a.small_rows = most_rows <= 16 || (heavy && most_rows <= kSmallRows) ? 16 : kSmallRows;
+    a.small_rows = small_rows;
     split_small((int64_t)c.P * c.H, reach(a.small_rows / c.G), &a);
     // (a workgroup a row, which the join takes for more than 32 parts, would be more threads than a launch has)
     if (rows > (1 << 22)) a.small_splits = std::min(a.small_splits, 30);

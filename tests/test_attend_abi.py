@@ -325,3 +325,23 @@ def test_one_row_is_dense_where_there_is_one_place():
     one = torch.zeros(128, dtype=torch.bfloat16).as_strided((1, 1, 1, 128), (0, 0, 0, 1))
     assert rkv._row_strides(one, "k") == (0, 0, 0)
     assert rkv._row_strides(torch.zeros((2, 3, 5, 256))[..., :128], "k") == (3840, 1280, 256)
+
+
+@pytest.mark.parametrize("P,G,T,max_new", [(2, 17, 2, 1), (3, 32, 2, 1), (4, 24, 3, 1), (2, 10, 4, 2), (5, 7, 15, 3)])
+def test_workspace_of_large_caches_has_many_rows_parts_only(lib, P, G, T, max_new):
+    """17 to 32 rows of queries over caches of 900 000 rows and more: no problem can have as few as the few-rows kernel takes there, so that no
+    part is its."""
+    p = block(shape(num_problems=P, kv_heads=2, q_heads=2 * G, n_tokens=1 << 20, budget=1 << 20))
+    for window in (0, 1000):
+        st, n = size(lib, p, att(tokens=T, max_new=max_new, window=window))
+        rows = T * 2 * G
+        up = lambda x: (x + 255) & ~255  # noqa: E731
+        assert st == rkv.RKV_OK and n in [0] + [up(rows * s * 512) + up(rows * s * 8) for s in range(2, 33)], n
+
+
+def test_workspace_of_large_caches_with_room_for_few_rows(lib):
+    """One token of some problems beside three of others: up to 16 rows are the few-rows kernel's, whose parts are there."""
+    p = block(shape(num_problems=5, kv_heads=2, q_heads=14, n_tokens=1 << 20, budget=1 << 20))
+    st, n = size(lib, p, att(tokens=11, max_new=3))
+    small = 5 * 2 * 16 * 512
+    assert st == rkv.RKV_OK and n > small
