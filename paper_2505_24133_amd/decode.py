@@ -95,9 +95,13 @@ class DecodeCache:
         held (or, with a window, its last rows and the first `sinks`); then the cache is compressed if it is full.
         Returns the attention's output [P, n, Hq, d]."""
         s = self.shape
-        P, n = q_new.shape[0], q_new.shape[1]
-        if P != s.num_problems or n < 1 or self.length + n > s.n_tokens:
-            raise ValueError(f"step takes tokens of {s.num_problems} problems, and room for {s.n_tokens - self.length} each is left")
+        P, n = s.num_problems, q_new.shape[1]
+        for t, heads in ((q_new, s.q_heads), (k_new, s.kv_heads), (v_new, s.kv_heads)):
+            if t.shape != (P, n, heads, s.head_dim):
+                raise ValueError(f"step takes tokens of {P} problems: q_new {(P, n, s.q_heads, s.head_dim)}, k_new and v_new "
+                                 f"{(P, n, s.kv_heads, s.head_dim)}, got {tuple(t.shape)}")
+        if n < 1 or self.length + n > s.n_tokens:
+            raise ValueError(f"step takes tokens of {P} problems, and room for {s.n_tokens - self.length} each is left")
         if cos.shape[0] < self.tokens_seen + n:
             raise ValueError(f"the rotation tables end at position {cos.shape[0]}, before the new tokens do")
         if self._counts is None:

@@ -114,3 +114,14 @@ def test_what_is_replaced_is_held_for_the_streams_that_use_it(reached, monkeypat
     cache.step(*tokens(1), *TABLES)
     assert reached.count("compress") == 1
     replaced(*lists)
+
+
+def test_tokens_of_other_shapes_are_refused(reached):
+    """Keys and values are those of the queries' tokens: as many of each problem, not only as many in all."""
+    cache = make(P=2, H=1, G=2)
+    q, k, v = tokens(3)
+    for bad in ((q, k.view(3, 2, 1, 128), v), (q, k, v.view(3, 2, 1, 128)), (q, k[:, :2], v), (q, k, v[:1]), (q[:, :, :1], k, v), (q.view(2, 6, 1, 128), k, v),
+                (q, k.flatten(0, 1), v), (q.flatten(0, 1), k, v), (q, k[..., :64], v)):
+        with pytest.raises(ValueError, match="step takes"):
+            cache.step(*bad, *TABLES)
+    assert reached == [] and cache.length == 0
