@@ -33,7 +33,8 @@ extern "C" {
  * Of a row's 128 channels the first rotary_dim are rotated in pairs, channel i with i + rotary_dim / 2, or 2 i with
  * 2 i + 1 if `interleaved`: (a, b) -> (a cos - b sin, b cos + a sin) with cos[position][i], sin[position][i] from tables
  * [table_rows, rotary_dim / 2] (fp32), in fp32 and rounded once.  A position past the table takes its last row; a token whose row is
- * not in [0, n_tokens), or whose page is not in [0, num_pages), is left out of the caches of keys and values.  q_out may be q_new.
+ * not in [0, n_tokens), or whose page is not in [0, num_pages), is left out of the caches of keys and values.  q_out may be q_new, with
+ * the same strides (others are refused).
  */
 typedef struct {
   int32_t tokens;            /* T >= 0 */

@@ -301,6 +301,8 @@ rkv_status rkv_cache_append_rotary(const rkv_params* prm, const rkv_rotary_param
   for (const void* x : {(const void*)k_cache, (const void*)v_cache, (const void*)q_cache, k_new, v_new, q_new, (const void*)q_out,
                         (const void*)r.cos, (const void*)r.sin})
     if (!aligned16(x)) return RKV_ERR_SHAPE;
+  // in place only where every row stays where it lies: a workgroup would write over a row that another one still has to read
+  if (q_out == q_new && ((r.tokens > 1 && a.qot != a.qnt) || (Hq > 1 && a.qoh != a.qnh))) return RKV_ERR_SHAPE;
   a.k_cache = static_cast<uint16_t*>(k_cache);
   a.v_cache = static_cast<uint16_t*>(v_cache);
   a.q_cache = static_cast<uint16_t*>(q_cache);

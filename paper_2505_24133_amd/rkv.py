@@ -560,7 +560,7 @@ def rkv_cache_append_rotary(shape: Shape, k_cache: torch.Tensor, v_cache: torch.
                             q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotate a ragged batch of new tokens (k_new, v_new [T, kv_heads, d], q_new [T, q_heads, d]; starts cuts them into the problems') by
     their positions seen[p] + j and write keys and values behind the held[p] rows of the caches and the last alpha queries of every
-    problem into q_cache (None: nowhere).  Returns the rotated queries (q_out, which may be q_new itself)."""
+    problem into q_cache (None: nowhere).  Returns the rotated queries (q_out, which may be q_new itself, row for row)."""
     if _append_rotary is None:
         load_library()
     # (as with rkv_cache_append: a call in order is checked and enqueued in native code)

@@ -345,3 +345,27 @@ def test_workspace_of_large_caches_with_room_for_few_rows(lib):
     st, n = size(lib, p, att(tokens=11, max_new=3))
     small = 5 * 2 * 16 * 512
     assert st == rkv.RKV_OK and n > small
+
+
+def test_queries_in_place_only_where_they_lie(lib):
+    """q_out may be q_new: then every row goes where it came from.  With other strides a row would be written over one still to be read."""
+    p = block(shape())                                                     # 32 query heads
+
+    def call(q, o, tokens=2, same=True, prm=p):
+        r = rkv.RkvRotaryParams(tokens=tokens, rotary_dim=128, table_rows=10, cos=0x1000, sin=0x1000, starts=0x1000, held=0x1000, seen=0x1000,
+                                q_stride_token=q[0], q_stride_head=q[1], o_stride_token=o[0], o_stride_head=o[1])
+        there = (FAKE, FAKE, None, FAKE, FAKE, FAKE, FAKE if same else ctypes.c_void_p(0x100000))
+        return lib.rkv_cache_append_rotary(ctypes.byref(prm), ctypes.byref(r), *there, None)
+
+    refused = [((4096, 128), (8192, 128)), ((8192, 256), (0, 0)), ((0, 0), (128, 256)), ((256, 512), (512, 512 * 8))]
+    for q, o in refused:
+        assert call(q, o) == rkv.RKV_ERR_SHAPE, (q, o)
+    if torch.cuda.is_available():
+        return                                                             # (what follows is enqueued where there is a GPU)
+    for q, o in (((4096, 128), (0, 0)), ((8192, 256), (8192, 256))):
+        assert call(q, o) == rkv.RKV_ERR_HIP
+    for q, o in refused[:2]:
+        assert call(q, o, same=False) == rkv.RKV_ERR_HIP
+    # strides of one token or one head say nothing
+    assert call((8192, 128), (4096, 128), tokens=1) == rkv.RKV_ERR_HIP
+    assert call((128, 1024), (128, 512), prm=block(shape(kv_heads=1, q_heads=1))) == rkv.RKV_ERR_HIP
