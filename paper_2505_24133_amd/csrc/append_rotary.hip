@@ -58,9 +58,9 @@ __global__ __launch_bounds__(256) void append_rotary_kernel(RotaryArgs a) {
   const int t = blockIdx.x;
   const int at = count_not_above(a.starts, a.P + 1, t) - 1;
   if (at < 0 || at >= a.P) return;                       // a token of no problem
-  const int j = t - a.starts[at];
+  const int first = clampi(a.starts[at], 0, a.T), end = clampi(a.starts[at + 1], 0, a.T), j = t - first;
   const int row = (int)((uint32_t)a.held[at] + (uint32_t)j), position = (int)((uint32_t)a.seen[at] + (uint32_t)j);   // (any list may wrap)
-  const bool kept = a.q_cache != nullptr && t >= (int64_t)a.starts[at + 1] - a.alpha;
+  const bool kept = a.q_cache != nullptr && t >= end - (int64_t)a.alpha;
   int64_t k_at = -1, v_at = -1;                          // where the row lies in the caches; -1: nowhere
   if (row >= 0 && row < a.N) {
     if (a.kl.table == nullptr) {

@@ -131,3 +131,21 @@ def test_graph():
         held += 1
         seen += 1
         k_new.normal_(generator=b.gen)
+
+
+def test_lists_that_begin_before_or_end_behind_the_tokens():
+    """starts below 0 and past T are taken as 0 and T, as attention takes them: the same rows, positions and kept queries."""
+    print("[gpu-case] append, starts outside the tokens", flush=True)
+    for new, outside in (([3, 6], [-2, 3, 12]), ([1, 20], [-(2 ** 31), 1, 2 ** 31 - 1]), ([12], [-5, 40])):
+        got = []
+        for starts in (outside, None):
+            b = Batch(2, 3, new, [64] * len(new), N=64, seed=11)
+            q = torch.randn((b.T, 6, 128), generator=b.gen, device="cuda").bfloat16()
+            kv = torch.randn((2, b.T, 2, 128), generator=b.gen, device="cuda").bfloat16()
+            ring = torch.zeros((b.P, 6, 4, 128), dtype=torch.bfloat16, device="cuda")
+            b.shape.alpha = 4
+            cos, sin = rkv.rotary_tables(100)
+            out = rkv.rkv_cache_append_rotary(b.shape, b.k, b.v, ring, kv[0], kv[1], q, cos, sin, b.starts if starts is None else int32(starts),
+                                              int32([5, 7][:b.P]), int32([30, 50][:b.P]))
+            got.append((b.k, b.v, ring, out))
+        assert all(torch.equal(x, y) for x, y in zip(*got)), new
