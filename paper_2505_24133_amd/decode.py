@@ -34,7 +34,8 @@ class DecodeCache:
         self.length = 0            # rows currently held per head
         self.tokens_seen = 0       # decode steps so far
         self.compressions = 0
-        self._counts = None        # row n: n for every problem (what the calls take as lengths), made at the first step
+        self._counts = None        # row n: n for every problem, made at the first step
+        self._count_of = {}        # its rows that steps have asked for
         self._starts = {}          # by new tokens a problem: where each problem's begin
         self._attend_room = {}     # and how much workspace their attention needs; one workspace serves them all
         self._attend_ws = None
@@ -49,6 +50,13 @@ class DecodeCache:
     @property
     def v(self) -> torch.Tensor:
         return self._v[self._cur]
+
+    def _count(self, n: int) -> torch.Tensor:
+        """n for every problem, as the calls take lengths and positions."""
+        row = self._count_of.get(n)
+        if row is None:
+            row = self._count_of[n] = self._counts[n]
+        return row
 
     def _let_go(self, *tensors) -> None:
         """Tensors that steps have used and that are about to be replaced.  Steps may have been made on other streams than the one they were
@@ -96,10 +104,10 @@ class DecodeCache:
         Returns the attention's output [P, n, Hq, d]."""
         s = self.shape
         P, n = s.num_problems, q_new.shape[1]
-        for t, heads in ((q_new, s.q_heads), (k_new, s.kv_heads), (v_new, s.kv_heads)):
-            if t.shape != (P, n, heads, s.head_dim):
-                raise ValueError(f"step takes tokens of {P} problems: q_new {(P, n, s.q_heads, s.head_dim)}, k_new and v_new "
-                                 f"{(P, n, s.kv_heads, s.head_dim)}, got {tuple(t.shape)}")
+        of_q, of_kv = (P, n, s.q_heads, s.head_dim), (P, n, s.kv_heads, s.head_dim)
+        if q_new.shape != of_q or k_new.shape != of_kv or v_new.shape != of_kv:
+            raise ValueError(f"step takes tokens of {P} problems: q_new {of_q}, k_new and v_new {of_kv}, "
+                             f"got {tuple(q_new.shape)}, {tuple(k_new.shape)} and {tuple(v_new.shape)}")
         if n < 1 or self.length + n > s.n_tokens:
             raise ValueError(f"step takes tokens of {P} problems, and room for {s.n_tokens - self.length} each is left")
         if cos.shape[0] < self.tokens_seen + n:
@@ -118,16 +126,16 @@ class DecodeCache:
         # what attention may refuse is refused here, and its output made: behind the append the query cache has lost the slots that the new
         # queries take, so nothing may fail there
         rkv._check_sight(window, sinks, n, scale, "DecodeCache.step")
-        out = torch.empty((P * n, s.q_heads, s.head_dim), dtype=torch.bfloat16, device=self.q_cache.device)
+        q = q_new.flatten(0, 1)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if self.q_cache.is_cuda and rkv._stream() not in self._streams:
             self._streams[rkv._stream()] = torch.cuda.current_stream()
-        starts, k, v = self._starts[n], self.k, self.v
+        starts, lens, k, v = self._starts[n], self._count(self.length + n), self.k, self.v
         # positions count from the last multiple of alpha, whose rows of the tables come first: the slots of the query cache go by them
         slot = self.tokens_seen % s.alpha
         at = self.tokens_seen - slot
-        q = rkv.rkv_cache_append_rotary(s, k, v, self.q_cache, k_new.flatten(0, 1), v_new.flatten(0, 1), q_new.flatten(0, 1), cos[at:], sin[at:],
-                                        starts, self._counts[self.length], self._counts[slot], interleaved=interleaved)
-        lens = self._counts[self.length + n]
+        q = rkv.rkv_cache_append_rotary(s, k, v, self.q_cache, k_new.flatten(0, 1), v_new.flatten(0, 1), q, cos[at:], sin[at:],
+                                        starts, self._count(self.length), self._count(slot), interleaved=interleaved)
         common = dict(window=window, sinks=sinks, scale=scale, max_new=n, ws=self._attend_ws, out=out)
         if self._groups is None:
             rkv.rkv_attend(s, q, k, v, starts, lens, **common)
@@ -137,7 +145,7 @@ class DecodeCache:
         self.tokens_seen += n
         if self.length >= s.n_tokens > s.budget:
             self.compress()
-        return out.view(P, n, s.q_heads, s.head_dim)
+        return out.view(of_q)
 
     def compress(self) -> None:
         s = self.shape

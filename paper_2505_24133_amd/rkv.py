@@ -614,10 +614,9 @@ def make_attend_workspace(shape: Shape, tokens: int, max_new: Optional[int] = No
 
 def _check_sight(window, sinks, max_new, scale, where: str) -> None:
     """What attention refuses of these, with the errors that it refuses them with."""
-    if not all(0 <= n <= _INT32_MAX for n in (window, sinks, max_new)):
+    if not (0 <= window <= _INT32_MAX and 0 <= sinks <= _INT32_MAX and 0 <= max_new <= _INT32_MAX):
         raise ValueError("window, sinks and max_new must be in 0 .. 2^31 - 1")
-    for n in (window, sinks, max_new):
-        operator.index(n)
+    operator.index(window), operator.index(sinks), operator.index(max_new)
     if scale is not None and not 0.0 < ctypes.c_float(scale).value < math.inf:
         raise RkvError(RKV_ERR_PARAM, where)
 
