@@ -19,6 +19,10 @@ import torch
 from . import rkv
 
 
+def _capturing(device) -> bool:
+    return device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+
+
 class DecodeCache:
     def __init__(self, shape: rkv.Shape, device="cuda", inplace: bool = False):
         self.shape = shape
@@ -41,6 +45,8 @@ class DecodeCache:
         self._attend_ws = None
         self._groups = None
         self._streams = {}         # by handle: the streams that steps were made on
+        self._captured = False     # whether one of them was captured into a graph,
+        self._kept = []            # and what that graph may use that has been replaced since
 
     @property
     def k(self) -> torch.Tensor:
@@ -60,7 +66,10 @@ class DecodeCache:
 
     def _let_go(self, *tensors) -> None:
         """Tensors that steps have used and that are about to be replaced.  Steps may have been made on other streams than the one they were
-        allocated on: their memory is not given out again before what those streams have been given by now is done."""
+        allocated on: their memory is not given out again before what those streams have been given by now is done.  A graph that a step was
+        captured into uses them as often as it is replayed: then they stay."""
+        if self._captured:
+            self._kept += tensors
         for t in tensors:
             for stream in self._streams.values():
                 t.record_stream(stream)
@@ -130,6 +139,7 @@ class DecodeCache:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if self.q_cache.is_cuda and rkv._stream() not in self._streams:
             self._streams[rkv._stream()] = torch.cuda.current_stream()
+        self._captured = self._captured or _capturing(self.q_cache.device)
         starts, lens, k, v = self._starts[n], self._count(self.length + n), self.k, self.v
         # positions count from the last multiple of alpha, whose rows of the tables come first: the slots of the query cache go by them
         slot = self.tokens_seen % s.alpha

@@ -125,3 +125,25 @@ def test_tokens_of_other_shapes_are_refused(reached):
         with pytest.raises(ValueError, match="step takes"):
             cache.step(*bad, *TABLES)
     assert reached == [] and cache.length == 0
+
+
+def test_what_a_captured_step_uses_is_kept(reached, monkeypatch):
+    """A graph goes on using the workspace and the groups that its step was captured with: they are not given back when they are replaced."""
+    capturing = [False]
+    monkeypatch.setattr(decode, "_capturing", lambda device: capturing[0])
+    cache = make()
+    room = {1: 1000, 3: 5000, 4: 9000}
+    monkeypatch.setattr(rkv, "rkv_attend_workspace_size", lambda shape, tokens, max_new, groups: room[max_new])
+    cache.step(*tokens(1), *TABLES)
+    cache.share_prompt([2], [1])
+    cache.step(*tokens(1), *TABLES)
+    first = [cache._attend_ws, *cache._groups]
+    cache.step(*tokens(3), *TABLES)
+    assert cache._kept == [] and cache._attend_ws is not first[0]        # no step was captured: the workspace has gone
+    first[0] = cache._attend_ws
+    capturing[0] = True
+    cache.step(*tokens(1), *TABLES)
+    capturing[0] = False
+    cache.step(*tokens(4), *TABLES)
+    cache.share_prompt([1, 1], [1, 1])
+    assert [id(t) for t in cache._kept] == [id(t) for t in first]

@@ -167,3 +167,34 @@ def test_a_replaced_workspace_is_not_given_out_under_a_step():
     assert not done.query()
     assert not {x.data_ptr() for x in given} & set(ptrs)
     torch.cuda.synchronize()
+
+
+def test_a_captured_step_and_longer_ones_behind_it():
+    """A captured step keeps its workspace: replays between and behind longer steps give what they gave, and write over nobody's memory."""
+    print("[gpu-case] captured step", flush=True)
+    s = shape(2, 2, 4, 3000, 2000)
+    cache, same = decode.DecodeCache(s), decode.DecodeCache(s)
+    cos, sin = rkv.rotary_tables(3000)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    t = {n: [torch.randn((2, n, h, 128), generator=gen, device="cuda").bfloat16() for h in (8, 2, 2)] for n in (700, 1, 90)}
+    for c in (cache, same):
+        c.step(*t[700], cos, sin)
+        c._attend_ws = None                                # (as if the prompt had come another way)
+        c.step(*t[1], cos, sin)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = cache.step(*t[1], cos, sin)
+    want = same.step(*t[1], cos, sin)
+    room = cache._attend_ws.numel()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    longer, want_longer = cache.step(*t[90], cos, sin), same.step(*t[90], cos, sin)
+    assert torch.equal(longer, want_longer) and cache._attend_ws.numel() > room
+    others = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in [room, room, room - 256, 4096, 4096] for _ in range(5)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(bool((x == 7).all()) for x in others)
+        assert torch.equal(cache.step(*t[1], cos, sin), same.step(*t[1], cos, sin))
