@@ -109,7 +109,8 @@ class DecodeCache:
              interleaved: bool = False, window: int = 0, sinks: int = 0, scale=None) -> torch.Tensor:
         """n new tokens of every problem: q_new [P, n, Hq, d], k_new, v_new [P, n, H, d], not rotated yet.  They are rotated by their
         positions (cos, sin: rotary_tables with a row for every position so far), appended, and attended over everything that is
-        held (or, with a window, its last rows and the first `sinks`); then the cache is compressed if it is full.
+        held (or, with a window, its last rows and the first `sinks`); then the cache is compressed if it is full.  The counts are the host's:
+        a step that is captured into a graph repeats its rows and positions, and needs one of as many tokens before the capture.
         Returns the attention's output [P, n, Hq, d]."""
         s = self.shape
         P, n = s.num_problems, q_new.shape[1]
@@ -121,6 +122,8 @@ class DecodeCache:
             raise ValueError(f"step takes tokens of {P} problems, and room for {s.n_tokens - self.length} each is left")
         if cos.shape[0] < self.tokens_seen + n:
             raise ValueError(f"the rotation tables end at position {cos.shape[0]}, before the new tokens do")
+        if (self._counts is None or n not in self._starts) and _capturing(self.q_cache.device):
+            raise RuntimeError(f"the first step of {n} tokens makes lists that a graph would fill only when it is replayed: make one before the capture")
         if self._counts is None:
             device = self.q_cache.device
             self._counts = torch.arange(s.n_tokens + 1, dtype=torch.int32, device=device)[:, None].expand(-1, P).contiguous()

@@ -147,3 +147,19 @@ def test_what_a_captured_step_uses_is_kept(reached, monkeypatch):
     cache.step(*tokens(4), *TABLES)
     cache.share_prompt([1, 1], [1, 1])
     assert [id(t) for t in cache._kept] == [id(t) for t in first]
+
+
+def test_a_first_step_is_not_captured(reached, monkeypatch):
+    """Lists that are made in a capture hold nothing before the first replay, and the steps behind it would read them."""
+    capturing = [True]
+    monkeypatch.setattr(decode, "_capturing", lambda device: capturing[0])
+    cache = make()
+    with pytest.raises(RuntimeError, match="before the capture"):
+        cache.step(*tokens(2), *TABLES)
+    capturing[0] = False
+    cache.step(*tokens(2), *TABLES)
+    capturing[0] = True
+    cache.step(*tokens(2), *TABLES)
+    with pytest.raises(RuntimeError, match="before the capture"):
+        cache.step(*tokens(1), *TABLES)
+    assert reached == ["append", "attend"] * 2 and cache.length == 4

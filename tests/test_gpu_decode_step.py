@@ -198,3 +198,15 @@ def test_a_captured_step_and_longer_ones_behind_it():
         torch.cuda.synchronize()
         assert torch.equal(out, want) and all(bool((x == 7).all()) for x in others)
         assert torch.equal(cache.step(*t[1], cos, sin), same.step(*t[1], cos, sin))
+
+
+def test_a_first_step_is_not_captured():
+    print("[gpu-case] first step in a capture", flush=True)
+    cache = decode.DecodeCache(shape(1, 1, 2, 40, 30))
+    cos, sin = rkv.rotary_tables(40)
+    t = [torch.zeros((1, 2, h, 128), dtype=torch.bfloat16, device="cuda") for h in (2, 1, 1)]
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="before the capture"):
+        with torch.cuda.graph(graph):
+            cache.step(*t, cos, sin)
+    assert cache.length == 0 and torch.isfinite(cache.step(*t, cos, sin).float()).all()
