@@ -301,3 +301,24 @@ def test_rows_that_see_nothing_under_any_window(window, sinks):
     for page in (0, 16):
         for new, lens in (([5, 8, 2, 8], [2, 1, 0, 200]), ([90, 40, 33], [33, 2, 0]), ([200, 3, 1], [150, 1, 120]), ([130], [7])):
             both(Batch(2, 4, new, lens, N=200, page=page, seed=25), window, sinks, where=f"{new} {lens} page {page}")
+
+
+@pytest.mark.parametrize("G,new,own", [
+    pytest.param(4, [1], [1151], id="one token in parts, and whole in a batch"),
+    pytest.param(8, [3], [997], id="a draft by itself, and beside prompts"),
+    pytest.param(5, [77], [2000], id="a chunk in parts"),
+])
+def test_a_problem_alone_and_in_batches(G, new, own):
+    """Parts and kernels go by the batch: a problem's answer keeps to its bounds in any, and so differs by twice as much at most."""
+    print(f"[gpu-case] attend alone and in batches {G} {new} {own}", flush=True)
+    first = new[0]
+    for others in ([1] * 3, [1] * 63, [first] * 40, [300, 1, 0, 17]):
+        counts = new + others
+        lens = own + [(40, 700, 1500)[i % 3] + n for i, n in enumerate(others)]
+        lens[0] += first
+        b = Batch(2, G, counts, lens, seed=26)
+        want = attend64(b)
+        check(run(b), want, f"beside {others}")
+        alone = rkv.Shape(num_problems=1, kv_heads=2, q_heads=2 * G, n_tokens=b.N, budget=b.N - 1)
+        got = rkv.rkv_attend(alone, b.q[:first], b.k[:1], b.v[:1], b.starts[:2], b.kv_len[:1], max_new=first, want_lse=True)
+        check(got, tuple(t[:first] for t in want), "alone")
