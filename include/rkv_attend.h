@@ -7,7 +7,11 @@
  * contents need not be preserved.  `rkv_params` describes the caches as it does there; of its fields these
  * calls read num_problems, kv_heads, q_heads, n_tokens, head_dim (128), the strides of k and v, and the paging fields (plus alpha
  * and the q_stride_* for the query cache).  What the compression step asks beyond that (budget, G * alpha <= 64, N <= 32768, ...) is
- * not asked: n_tokens may be up to 2^24, G anything.
+ * not asked: n_tokens may be up to 2^24, q_heads up to 4096, in groups of any size, num_problems * kv_heads up to 2^22.  Of new tokens the
+ * append takes T <= 2^23, attention T * ceil(q_heads / 8) < 2^24.  More is RKV_ERR_UNSUPPORTED.
+ *
+ * Strides of token arrays that are 0, 0 say dense; of others the one of a dimension with several entries is positive (arrays that are
+ * broadcast are refused), and rows lie on 16 bytes.
  *
  * A batch is ragged: `starts` [P + 1] (int32, device, ascending) cuts the T new tokens into those of problem 0, 1, ...; a
  * problem may have none.  Rows of the token arrays behind starts[P] are neither read nor written.  Values that lie in

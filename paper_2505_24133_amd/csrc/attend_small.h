@@ -6,8 +6,9 @@
 // S^T = K Q^T by MFMA 16x16x32 puts a query in a lane and rows in its registers, so that the softmax is register arithmetic and two lane
 // exchanges, and its result is, without any movement, the second operand of O^T += V^T P^T; V^T comes out of LDS by the transposing
 // read.  The waves are joined through LDS, workgroups of a unit by attend_join.hip.
-// 64 sequences of 1152 rows, 8 KV heads (303 MB): 49 us, 6.2 TB/s, 57 (5.3) with caches that were not used before; one sequence of 32768 rows 24 us
-// (5.6 TB/s) and the join; of 1152 rows 5 us, most of it the reads that follow each other (starts and length, page, rows).
+// 64 sequences of 1152 rows, 8 KV heads (303 MB): 48 to 51 us, 6.0 to 6.3 TB/s, 57 (5.3) with caches that were not used before, where nothing
+// but reads of 8 GiB reach 6.0 TB/s; one sequence of 32768 rows 24 us (5.6 TB/s) and the join; of 1152 rows 5 us, most of it the reads that
+// follow each other (starts, then the length, the page, the rows).
 #pragma once
 
 #include "attend_internal.h"
@@ -140,7 +141,8 @@ __device__ __forceinline__ void attend(const AttendArgs& a, int block, Lds<MT>& 
         add += x[i];
       }
       sum[m] = sum[m] * fade + add;                              // of this lane's rows; lanes are added up at the end
-      // the weights as bf16, for the second product
+      // the weights as bf16, which the matrix pipe takes: o moves by at most 2^-8 sum w |v| (0.0020 relative to 64 bits where 32-bit weights
+      // have 0.0017, most of either o's own rounding); the sum is that of the weights before, for lse has 32 bits
 #pragma unroll
       for (int i = 0; i < 8; ++i) pf[m].b[i] = (__bf16)x[i];
 #pragma unroll

@@ -6,13 +6,21 @@
 // 32x32x16: a lane has one query and half of the step's rows, so that maxima and sums are register arithmetic and one exchange
 // between the halves of the wave, and the weights are, without any movement, the second operand of O^T += V^T P^T.  V^T comes out of
 // LDS by the transposing read.  The next step's scores are formed beside this step's exponentials, and two workgroups share a compute unit, so
-// that one's products run beside the other's maxima.  Everything stays in 256 registers: one that is spilled is read back behind a
-// wait for all copies under way (12 % of a long prompt).
-// The largest prompts run at 1.03 PFLOP/s (three of up to 15000 tokens, 32 heads on 8: 600 us) where a library product of 8192^3 reaches
-// 1.30 and the same matrix and vector instructions with nothing to wait for 1.6; without the copies it would be 540 us, without
-// the reads of LDS too 489: LDS delivers 128 bytes a cycle, just what 32 query rows a wave use of it, and the clock falls with the power
-// that the products draw.  48 query rows a wave (16x16x32) win 3 % there and lose 7 to 18 where there are edges or few tiles; 64, one
-// wave a SIMD, take 1.5 times as long.
+// that one's products run beside the other's maxima.  Two workgroups leave a lane 256 registers, and the loop stays in them: one that is
+// spilled is read back behind a wait for all copies under way (12 % of a long prompt).  Beside few-rows units (attend_beside.hip) 15 to 31
+// scalar registers spill to vector registers, and for shared prefixes in contiguous caches four vector registers to memory, where values that
+// are not finite are taken out.
+//
+// The weights are the second product's operand, and the matrix pipe takes 16 bits at this rate: they are rounded to bf16, which moves o by
+// at most 2^-8 sum w |v| (measured against 64 bits: 0.0021 to 0.0023 relative where a plain form with 32-bit weights has 0.0017, most of
+// either o's own rounding).  The sum l adds them before the rounding, for lse has 32 bits; and as the reference may lag behind the maximum by
+// 2^8, the largest weight is rounded as well.  M, l and o are held in 32 bits.
+//
+// The largest prompts run at 0.97 to 1.05 PFLOP/s (three of up to 15000 tokens, 32 heads on 8: 590 to 640 us by the card), where a library
+// product of 8192^3 reaches 1.22 to 1.30 and the loop's matrix and vector instructions by themselves, in registers, 1.56: the matrix pipe is
+// busy in 55 % of the cycles.  At its full rate 32 query rows a wave would read 120 of the 128 bytes a cycle that LDS delivers, and the
+// clock falls with the power that the products draw.  48 query rows a wave (16x16x32) win 3 % there and lose 7 to 18 where there are
+// edges or few tiles; 64, one wave a SIMD, take 1.5 times as long.
 #pragma once
 
 #include <type_traits>
