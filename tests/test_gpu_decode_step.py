@@ -146,6 +146,7 @@ def test_a_replaced_workspace_is_not_given_out_under_a_step():
     cos, sin = rkv.rotary_tables(4000)
     t = {n: [torch.zeros((1, n, h, 128), dtype=torch.bfloat16, device="cuda") for h in (4, 1, 1)] for n in (1, 60)}
     assert rkv.rkv_attend_workspace_size(s, 60, 60, 1) > rkv.rkv_attend_workspace_size(s, 1, 1, 1)
+    decode.DecodeCache(s).step(*t[60], cos, sin)           # (its kernels are loaded now)
     cache.step(*t[1], cos, sin)
     cache.share_prompt([1], [1])
     cache.step(*t[1], cos, sin)
@@ -155,7 +156,7 @@ def test_a_replaced_workspace_is_not_given_out_under_a_step():
     other = torch.cuda.Stream()
     other.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(other):
-        torch.cuda._sleep(200_000_000)                     # (some 100 ms, which end by themselves)
+        torch.cuda._sleep(200_000_000)                     # (a time that ends by itself)
         cache.step(*t[1], cos, sin)
         done = torch.cuda.Event()
         done.record()
@@ -164,7 +165,8 @@ def test_a_replaced_workspace_is_not_given_out_under_a_step():
     with torch.cuda.stream(other):
         cache.step(*t[60], cos, sin)
     given = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(20)]
-    assert not done.query()
+    if done.query():
+        pytest.skip("the other stream was through before the memory was asked for")
     assert not {x.data_ptr() for x in given} & set(ptrs)
     torch.cuda.synchronize()
 
